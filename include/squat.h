@@ -51,6 +51,8 @@ typedef enum { SQUAT_KEYS = 0, SQUAT_VALUES = 1 } squat_kind;
                                        * address outside the buffer or on-chip region it belongs to; the access was skipped      */
 #define SQUAT_FLAG_DEVICE_TIMEOUT 8u /* a bounded wait on the tensor core inside squat_quantize_keys ran
                                        * out: that call's outputs are invalid (the kernel still ends)  */
+#define SQUAT_FLAG_PAGES 32u          /* a slot, page number, length or row range that a paged call read on the device lies
+                                       * outside its limits: what it names was neither read nor written */
 
 /* Opaque per-layer state: the update matrices of every KV head (shared by all samples of a
  * batch, Appendix C) plus the scratch the subspace build needs.  Owns device memory. */
@@ -357,6 +359,129 @@ int squat_decode_attention_pre_rope(const void *q, int q_dtype, int batch, int n
                                     int group_size, const void *k_res, const void *v_res, int res_dtype, int n_res,
                                     float softmax_scale, const float *rope_table, int table_positions,
                                     long long first_pos, float *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rotary position embedding with several axes.  Keys that are stored after the embedding, and the queries that the readers
+ * take "already rotated at their own position", get their positions here.  Text has one axis; a token of an image or a video
+ * has a position in time, height and width, and each axis turns its own range of channel pairs.
+ *
+ *   pair i = channels (i, i + n_pairs), i < n_pairs; channels from 2 n_pairs on are left as they are
+ *   angle  = positions[axis of i][token] * base^(-i / n_pairs)
+ *   (x_i, x_{i + n_pairs}) <- (x_i cos - x_{i + n_pairs} sin, x_{i + n_pairs} cos + x_i sin);   inverse: sin negated
+ *
+ * With one axis of d / 2 pairs this is the embedding of squat_rope_table_fill.  The inverse turns keys back to what they were
+ * before the embedding, and is the gradient of the forward call.
+ *
+ * squat_rope_plan_fill (host): sections[a] is the number of pairs of axis a, in order; their sum n_pairs is a multiple of 8
+ * and at most d / 2 (other sums: SQUAT_ERR_SHAPE).  base > 1.  The angle of a pair for one position is kept as a 64-bit fraction
+ * of a turn, and its product with a position modulo 2^64 is the rest of the angle: far positions lose nothing.  The caller keeps
+ * the plan; squat_rope_apply reads it during the call.
+ */
+#define SQUAT_ROPE_MAX_AXES 4
+typedef struct {
+    unsigned long long turn[64];       /* angle per position, in 2^-64 turns */
+    unsigned char axis[64];
+    int n_pairs, n_axes;
+} squat_rope_plan;
+int squat_rope_plan_fill(double base, int head_dim, const int *sections, int n_axes, squat_rope_plan *plan);
+
+/*
+ * Rotates queries and keys of n_tokens tokens in one launch.
+ *   positions      device, [n_axes, n_tokens]: int32 (positions64 = 0) or int64 (1), axis_stride elements between axes.
+ *   q, k           [n_tokens, heads, d], d contiguous, element strides given (multiples of 16 bytes); dtype for both.  k may be
+ *                  NULL (n_k_heads = 0), and so may q.
+ *   q_out, k_out   their own strides; q_out = q with equal strides rotates in place, other overlaps are not allowed.
+ * Arithmetic is float32, rounded once to the output's type.  head_dim must be 128.
+ */
+int squat_rope_apply(const squat_rope_plan *plan, const void *positions, int positions64, long long axis_stride, int n_tokens,
+                     int head_dim, int dtype, int inverse,
+                     const void *q, int n_q_heads, long long q_stride_t, long long q_stride_h,
+                     void *q_out, long long q_out_stride_t, long long q_out_stride_h,
+                     const void *k, int n_k_heads, long long k_stride_t, long long k_stride_h,
+                     void *k_out, long long k_out_stride_t, long long k_out_stride_h, void *stream);
+
+/*
+ * A paged cache.  A page holds page_tokens tokens of every KV head in the layout of the cache above: token t of page p and
+ * head h sits at token index p * page_stride + h * head_stride + t (strides in tokens, multiples of group_size; dense pages:
+ * page_stride = n_kv_heads * page_tokens, head_stride = page_tokens).  A token index moves a code pointer by d * bits / 8 bytes, key
+ * metadata by d elements for every group_size tokens and value metadata by d / group_size elements.  page_tokens is a multiple of
+ * group_size; the pool has fewer than 2^31 slots.  meta16 = 1: scales and zero-points are binary16.  The struct is read on the host
+ * during a call; the memory is the caller's.  A sequence's tokens go to any pages in any order; slot p * page_tokens + t names a
+ * place in the pool.
+ */
+typedef struct {
+    unsigned char *k_codes;
+    void *k_scales, *k_zeros;
+    unsigned char *v_codes;
+    void *v_scales, *v_zeros;
+    long long page_stride, head_stride;
+    int n_pages, page_tokens, n_kv_heads, head_dim, bits, group_size, meta16;
+} squat_page_pool;
+
+/*
+ * Quantizes n_tokens new keys and / or values into pages: steps 2 and 3 with the places that an engine's allocator has chosen.
+ *   k, v      [n_tokens, n_kv_heads, d], d contiguous, element strides given (multiples of 16 bytes).  Either may be NULL.
+ *   slots     device int32 [n_tokens / group_size]: the slot of each group's first token, a multiple of group_size; a negative
+ *             slot is a group that is not written (padding).  The slots of one call differ from each other.  The groups may
+ *             belong to any number of sequences.  A slot outside the pool sets SQUAT_FLAG_PAGES and its group is not written.
+ *   s         the layer's update matrices: keys as squat_quantize_keys, through `workspace` (device, 256-byte aligned, at
+ *             least squat_pages_write_workspace_bytes(pool, n_tokens); nothing is kept in it between calls).  NULL: keys rounded
+ *             to nearest without error feedback (W = 0), in one launch with the values and without a workspace.
+ * Values, and keys with s = NULL: scale = (max - min) * RN(1 / L) in binary32 (a product, whose last bit may differ from the
+ * quotient that squat_quantize_values and squat_quantize_keys store), zero = min; with meta16 both rounded to binary16.  Codes
+ * are decided by the stored grid: values as c = clamp(rint((x - zero) / scale), 0, L) in binary32, operation by operation, keys as real
+ * arithmetic would, ties to even.  n_tokens is a multiple of group_size.  Status word: as the quantizers set it.
+ */
+size_t squat_pages_write_workspace_bytes(const squat_page_pool *pool, int n_tokens);
+int squat_pages_write(const squat_subspace *s, const squat_page_pool *pool, const int *slots, int n_tokens, int dtype,
+                      const void *k, long long k_stride_t, long long k_stride_h, const void *v, long long v_stride_t,
+                      long long v_stride_h, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Reads groups of tokens back from pages (squat_dequantize with places): row i * group_size + t of k_out and v_out
+ * [n_tokens, n_kv_heads, d] becomes the token at slots[i] + t.  Rows of a negative slot are left as they were, and so are those of a
+ * slot outside the pool (SQUAT_FLAG_PAGES).  Either output may be NULL.  Element strides are multiples of 16 bytes.
+ */
+int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens, int out_dtype,
+                     void *k_out, long long k_stride_t, long long k_stride_h,
+                     void *v_out, long long v_stride_t, long long v_stride_h, void *stream);
+
+/*
+ * Attention of new tokens over the pages: one token per sequence (a decode step), a few (drafted tokens that are looked at
+ * together), chunks of prompts, or all of these in one call.  Sequence i has n_i = q_start[i + 1] - q_start[i] new queries,
+ * cached_len[i] tokens in pages and new_len[i] rows in full precision (its residual buffer and the new tokens' own rows).  Query j
+ * of sequence i sees all its cached tokens and, of its rows, with causal = 1 the first new_len[i] - n_i + j + 1 (the queries
+ * are the last n_i rows), with causal = 0 all.  out = softmax(softmax_scale q K^T) V over what it sees; zero (lse: -infinity)
+ * where it sees nothing.
+ *
+ *   q, out       [n_q, n_q_heads, d] bf16, d contiguous, element strides (multiples of 8 elements).
+ *   q_start      device int32 [n_seqs + 1], not decreasing, within [0, n_q].  Rows of `out` that belong to no sequence are left as
+ *                they were.
+ *   cached_len   device int32 [n_seqs], multiples of group_size, at most table_stride * page_tokens.
+ *   page_table   device int32 [n_seqs, table_stride]: page j holds the sequence's tokens j * page_tokens on.  Entries past a
+ *                sequence's length are not used.
+ *   k_new, v_new [n_new, n_kv_heads, d] bf16, d contiguous, element strides (multiples of 8 elements); sequence i's rows begin at
+ *                new_start[i] (device int32), new_len[i] of them (device int32).  n_new = 0: all four may be NULL.
+ *   max_q        the largest n_i, a host value that chooses the kernel; results are right for other values too.
+ *   softmax_scale  0: 1 / sqrt(d).
+ *   lse          NULL, or float32 [n_q, n_q_heads]: natural logarithm of the softmax's denominator.
+ *   workspace    device, 256-byte aligned, at least squat_chunk_attention_workspace_bytes(...); nothing is kept in it between
+ *                calls.  Calls that may run at the same time need workspaces of their own.
+ * Everything that changes from step to step is read on the device, so a captured call can be replayed with other lengths,
+ * pages and row ranges (n_q, n_seqs and max_q as captured).  A length or row range outside its limits sets SQUAT_FLAG_PAGES and is
+ * cut to them; for a page number outside the pool (the flag too) the result of that sequence is not defined.
+ * Scores, softmax and sums are float32.  Keys, values, queries and weights enter the tensor cores in binary16 (11 significant
+ * bits: codes, bf16 rows and queries exactly, dequantized values and weights rounded) where their magnitudes allow it, else in
+ * bf16.
+ */
+size_t squat_chunk_attention_workspace_bytes(int n_q, int n_q_heads, int n_kv_heads, int max_q);
+int squat_chunk_attention(const void *q, int n_q, int n_q_heads, long long q_stride_t, long long q_stride_h,
+                          const squat_page_pool *pool, int n_seqs, const int *q_start, const int *cached_len,
+                          const int *page_table, int table_stride, const void *k_new, const void *v_new, int n_new,
+                          long long k_new_stride_t, long long k_new_stride_h, long long v_new_stride_t, long long v_new_stride_h,
+                          const int *new_start, const int *new_len, int max_q, int causal, float softmax_scale,
+                          void *out, long long out_stride_t, long long out_stride_h, float *lse,
+                          void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Gram matrices of the stacked prompt queries without any allocation.  (The paper has no counterpart:

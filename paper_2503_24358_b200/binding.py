@@ -21,6 +21,7 @@ LIB_PATH = os.environ.get("SQUAT_LIBRARY") or os.path.join(_HERE, "libsquat.so")
 SQUAT_F32, SQUAT_BF16 = 0, 1
 SQUAT_KEYS, SQUAT_VALUES = 0, 1
 FLAG_NONFINITE, FLAG_ZERO_RANGE, FLAG_NO_CONVERGE, FLAG_DEVICE_TIMEOUT, FLAG_BOUNDS = 1, 2, 4, 8, 16
+FLAG_PAGES = 32
 
 EXPORTED_SYMBOLS = (
     "squat_subspace_create", "squat_subspace_destroy", "squat_build_subspace", "squat_subspace_export",
@@ -31,6 +32,8 @@ EXPORTED_SYMBOLS = (
     "squat_rope_table_floats", "squat_rope_table_fill", "squat_decode_attention_pre_rope",
     "squat_decode_attention_ex", "squat_build_subspace_from_gram", "squat_build_subspace_power", "squat_write_path_host_ex", "squat_build_subspace_power_from_gram", "squat_quantize_keys_m16", "squat_quantize_values_m16", "squat_dequantize_m16",
     "squat_fp32_peak_probe", "squat_append_window_host", "squat_subspace_select_key_kernel", "squat_checked_selftest",
+    "squat_rope_plan_fill", "squat_rope_apply", "squat_pages_write_workspace_bytes", "squat_pages_write", "squat_pages_read",
+    "squat_chunk_attention_workspace_bytes", "squat_chunk_attention",
 )
 
 _lib = None
@@ -93,6 +96,16 @@ def _load():
         lib.squat_subspace_select_key_kernel.argtypes = [vp, i, c.POINTER(i)]
         lib.squat_checked_selftest.argtypes = [vp, c.POINTER(i)]
         lib.squat_fp32_peak_probe.argtypes = [i, i, vp, c.POINTER(ll), vp]
+        lib.squat_rope_plan_fill.argtypes = [dbl, i, vp, i, vp]
+        lib.squat_rope_apply.argtypes = [vp, vp, i, ll, i, i, i, i] + [vp, i, ll, ll, vp, ll, ll] * 2 + [vp]
+        lib.squat_pages_write_workspace_bytes.argtypes = [vp, i]
+        lib.squat_pages_write_workspace_bytes.restype = c.c_size_t
+        lib.squat_pages_write.argtypes = [vp, vp, vp, i, i, vp, ll, ll, vp, ll, ll, vp, c.c_size_t, vp]
+        lib.squat_pages_read.argtypes = [vp, vp, i, i, vp, ll, ll, vp, ll, ll, vp]
+        lib.squat_chunk_attention_workspace_bytes.argtypes = [i, i, i, i]
+        lib.squat_chunk_attention_workspace_bytes.restype = c.c_size_t
+        lib.squat_chunk_attention.argtypes = [vp, i, i, ll, ll, vp, i, vp, vp, vp, i, vp, vp, i, ll, ll, ll, ll, vp, vp, i, i,
+                                              c.c_float, vp, ll, ll, vp, vp, c.c_size_t, vp]
         lib.squat_get_device_status.argtypes = [vp, c.POINTER(c.c_uint), i]
         lib.squat_kernel_launch_count.restype = c.c_ulonglong
         lib.squat_status_string.argtypes = [i]
@@ -563,6 +576,204 @@ def squat_decode_attention_pre_rope(q: torch.Tensor, k_codes, k_scales, k_zeros,
         csb, csh, bits, group_size, _opt(k_res, "k_res"), _opt(v_res, "v_res"), _dtype_code(k_res) if n_res else SQUAT_F32,
         n_res, _dev(rope_table, "rope_table"), int(table_positions), int(first_pos), _dev(out, "out"), _dev(workspace, "workspace"),
         workspace.numel() * workspace.element_size(), _stream(stream)), "squat_decode_attention_pre_rope")
+
+
+class RopePlan:
+    """Angles and axes of a rotary embedding (squat_rope_plan_fill): sections[a] channel pairs turn by positions of axis a.  Made
+    once per model; squat_rope_apply takes it."""
+
+    class _Struct(ctypes.Structure):
+        _fields_ = [("turn", ctypes.c_ulonglong * 64), ("axis", ctypes.c_ubyte * 64), ("n_pairs", ctypes.c_int), ("n_axes", ctypes.c_int)]
+
+    def __init__(self, sections=(64,), base: float = 10000.0, head_dim: int = 128):
+        self.sections, self.base, self.head_dim = tuple(int(n) for n in sections), float(base), int(head_dim)
+        self._plan = RopePlan._Struct()
+        n = (ctypes.c_int * max(1, len(self.sections)))(*self.sections)
+        _check(_load().squat_rope_plan_fill(self.base, self.head_dim, ctypes.addressof(n), len(self.sections),
+                                            ctypes.addressof(self._plan)), "squat_rope_plan_fill")
+        self.address = ctypes.addressof(self._plan)
+
+
+def _rows(x, name):
+    """Address and strides of [tokens, heads, d]."""
+    if x.dim() != 3 or (x.stride(2) != 1 and x.shape[2] != 1):
+        raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous last dim")
+    st, sh, _ = x.stride()
+    return _dev(x, name), st, sh
+
+
+def squat_rope_apply(plan: RopePlan, positions: torch.Tensor, q: torch.Tensor = None, k: torch.Tensor = None,
+                     q_out: torch.Tensor = None, k_out: torch.Tensor = None, inverse: bool = False, stream=None):
+    """Rotates q [tokens, n_q_heads, d] and / or k [tokens, n_kv_heads, d] by their positions [n_axes, tokens] (int32 or int64; one
+    axis may come as [tokens]) into q_out and k_out; without an output tensor in place."""
+    if positions.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"positions must be int32 or int64, not {positions.dtype}")
+    if positions.dim() == 1:
+        positions = positions.unsqueeze(0)
+    x = q if q is not None else k
+    if x is None:
+        return
+    T, d = x.shape[0], x.shape[2]
+    if tuple(positions.shape) != (len(plan.sections), T) or (T > 1 and positions.stride(1) != 1):
+        raise ValueError("positions must be [n_axes, tokens] with contiguous tokens")
+    args = []
+    for a, b, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if a is None:
+            args += [None, 0, 0, 0, None, 0, 0]
+            continue
+        b = a if b is None else b
+        if a.shape != b.shape or a.dtype != x.dtype or b.dtype != x.dtype or a.shape[0] != T or a.shape[2] != d:
+            raise ValueError("q, k and their outputs must have one dtype, token count and head_dim, and outputs their input's shape")
+        pa, ta, ha = _rows(a, name)
+        args += [pa, a.shape[1], ta, ha, *_rows(b, name + "_out")]
+    _check(_load().squat_rope_apply(plan.address, _dev(positions, "positions"), positions.dtype == torch.int64, positions.stride(0), T,
+                                    d, _dtype_code(x), 1 if inverse else 0, *args, _stream(stream)), "squat_rope_apply")
+
+
+class PagePool:
+    """The pages of one layer's paged cache (squat_page_pool): six tensors that the caller owns or PagePool.empty makes.
+
+    k_codes, v_codes   uint8 [n_pages, n_kv_heads, page_tokens, head_dim * bits / 8]
+    k_scales, k_zeros  [n_pages, n_kv_heads, page_tokens / group_size, head_dim], float32 or float16
+    v_scales, v_zeros  [n_pages, n_kv_heads, page_tokens, head_dim / group_size], the same type
+    Pages and heads may be strided (pages of all layers side by side), all six alike."""
+
+    class _Struct(ctypes.Structure):
+        _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_scales", "k_zeros", "v_codes", "v_scales", "v_zeros")] + \
+                   [("page_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong)] + \
+                   [(n, ctypes.c_int) for n in ("n_pages", "page_tokens", "n_kv_heads", "head_dim", "bits", "group_size", "meta16")]
+
+    def __init__(self, k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros):
+        tensors = (k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros)
+        if any(t.dim() != 4 for t in tensors):
+            raise ValueError("the six tensors of a pool are [n_pages, n_kv_heads, ...]")
+        n, H, P, row = k_codes.shape
+        d, groups = k_scales.shape[3], k_scales.shape[2]
+        if groups < 1 or P % groups or d < 1 or row * 8 % d:
+            raise ValueError("codes and scales of the keys do not belong together")
+        G, bits = P // groups, row * 8 // d
+        meta16 = _meta16(k_scales, k_zeros)
+        if k_codes.dtype != torch.uint8 or v_codes.dtype != torch.uint8 or _meta16(v_scales, v_zeros) != meta16:
+            raise ValueError("codes must be uint8, scales and zero-points of one type")
+        shapes = {"k_scales": (n, H, groups, d), "k_zeros": (n, H, groups, d), "v_codes": (n, H, P, row), "v_scales": (n, H, P, d // G),
+                  "v_zeros": (n, H, P, d // G)}
+        for (name, want), t in zip(shapes.items(), tensors[1:]):
+            if tuple(t.shape) != want:
+                raise ValueError(f"{name} must be {list(want)}, not {list(t.shape)}")
+        ps, hs = (k_codes.stride(i) // row if k_codes.shape[i] > 1 else P * (H if i == 0 else 1) for i in (0, 1))
+        for t, per_token in zip(tensors, (row, d / G, d / G, row, d // G, d // G)):
+            for i, stride in ((0, ps), (1, hs)):
+                if t.shape[i] > 1 and t.stride(i) != stride * per_token:
+                    raise ValueError("pages and heads of the six tensors must have the same strides in tokens")
+            if t.numel() and (t.stride(3) != 1 and t.shape[3] > 1 or t.shape[2] > 1 and t.stride(2) != t.shape[3]):
+                raise ValueError("a head's part of a page must be contiguous")
+            if t.device != k_codes.device:
+                raise ValueError("the six tensors of a pool must be on one device")
+        self.tensors = tensors
+        self.k_codes, self.k_scales, self.k_zeros, self.v_codes, self.v_scales, self.v_zeros = tensors
+        self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, self.bits, self.group_size = n, P, H, d, bits, G
+        self.device = k_codes.device
+        names = ("k_codes", "k_scales", "k_zeros", "v_codes", "v_scales", "v_zeros")
+        self._pool = PagePool._Struct(*(_dev(t, m) if t.numel() else None for t, m in zip(tensors, names)), ps, hs, n, P, H, d, bits, G, int(meta16))
+        self.address = ctypes.addressof(self._pool)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_tokens: int, n_kv_heads: int, bits: int, group_size: int, head_dim: int = 128,
+              meta_dtype: torch.dtype = torch.float32, device="cuda"):
+        """A pool of its own memory; codes and metadata are zero until they are written."""
+        z = lambda *shape, dtype=meta_dtype: torch.zeros((n_pages, n_kv_heads, *shape), dtype=dtype, device=device)  # noqa: E731
+        row, keys, values = head_dim * bits // 8, (page_tokens // group_size, head_dim), (page_tokens, head_dim // group_size)
+        return cls(z(page_tokens, row, dtype=torch.uint8), z(*keys), z(*keys), z(page_tokens, row, dtype=torch.uint8), z(*values), z(*values))
+
+
+def _int32(t, name, numel):
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {numel} elements")
+    return _dev(t, name)
+
+
+def _pool_rows(pool, slots, tensors, names):
+    """Token count and dtype of the key and value rows that come with `slots`, and their addresses and strides."""
+    T = slots.numel() * pool.group_size
+    args, dtype = [], None
+    for x, name in zip(tensors, names):
+        if x is None:
+            args += [None, 0, 0]
+            continue
+        if tuple(x.shape) != (T, pool.n_kv_heads, pool.head_dim):
+            raise ValueError(f"{name} must be [len(slots) * group_size, n_kv_heads, head_dim]")
+        if dtype is not None and x.dtype != dtype:
+            raise ValueError(f"{names[0]} and {names[1]} must have one dtype")
+        dtype = x.dtype
+        args += _rows(x, name)
+    return T, dtype, args
+
+
+def squat_pages_write_workspace_bytes(pool: PagePool, n_tokens: int) -> int:
+    return int(_load().squat_pages_write_workspace_bytes(pool.address, n_tokens))
+
+
+def squat_pages_write(pool: PagePool, slots: torch.Tensor, k: torch.Tensor = None, v: torch.Tensor = None, s: Subspace = None,
+                      workspace: torch.Tensor = None, stream=None):
+    """Quantizes k and / or v [tokens, n_kv_heads, d] into the pool: group i of group_size tokens goes to slots[i] (int32, page *
+    page_tokens + token; negative: not written).  With a Subspace the keys are quantized with its error feedback, through a
+    workspace (CUDA uint8) of squat_pages_write_workspace_bytes(pool, tokens); without one they are rounded to nearest."""
+    T, dtype, args = _pool_rows(pool, slots, (k, v), ("k", "v"))
+    if dtype is None:
+        return
+    x = k if k is not None else v
+    _check(_load().squat_pages_write(None if s is None else s.handle.value, pool.address, _int32(slots, "slots", slots.numel()), T, _dtype_code(x),
+                                     *args, None if workspace is None else _dev(workspace, "workspace"),
+                                     0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
+           "squat_pages_write")
+
+
+def squat_pages_read(pool: PagePool, slots: torch.Tensor, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
+    """Dequantizes the groups at `slots` into rows of k_out and / or v_out [tokens, n_kv_heads, d] (float32 or bfloat16)."""
+    T, dtype, args = _pool_rows(pool, slots, (k_out, v_out), ("k_out", "v_out"))
+    if dtype is None:
+        return
+    x = k_out if k_out is not None else v_out
+    _check(_load().squat_pages_read(pool.address, _int32(slots, "slots", slots.numel()), T, _dtype_code(x), *args, _stream(stream)),
+           "squat_pages_read")
+
+
+def squat_chunk_attention_workspace_bytes(n_q: int, n_q_heads: int, n_kv_heads: int, max_q: int) -> int:
+    return int(_load().squat_chunk_attention_workspace_bytes(n_q, n_q_heads, n_kv_heads, max_q))
+
+
+def squat_chunk_attention(q: torch.Tensor, pool: PagePool, q_start: torch.Tensor, cached_len: torch.Tensor, page_table: torch.Tensor,
+                          out: torch.Tensor, workspace: torch.Tensor, max_q: int, k_new: torch.Tensor = None, v_new: torch.Tensor = None,
+                          new_start: torch.Tensor = None, new_len: torch.Tensor = None, causal: bool = True, softmax_scale: float = 0.0,
+                          lse: torch.Tensor = None, stream=None):
+    """Attention of new tokens over the pages and the rows in full precision.  q, out [n_q, n_q_heads, d] bfloat16; sequence i's
+    queries are q[q_start[i]:q_start[i + 1]], its cached tokens the first cached_len[i] of pages page_table[i], its rows
+    k_new / v_new[new_start[i]:][:new_len[i]] (bfloat16 [rows, n_kv_heads, d]).  Index tensors are int32 on the device and are
+    read there; max_q is the largest number of queries of a sequence.  workspace: CUDA uint8 of
+    squat_chunk_attention_workspace_bytes(n_q, n_q_heads, n_kv_heads, max_q)."""
+    n_seqs = cached_len.numel()
+    if q.dim() != 3 or q.shape != out.shape or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.shape[2] != pool.head_dim:
+        raise ValueError("q and out must be bfloat16 [n_q, n_q_heads, head_dim]")
+    if page_table.dim() != 2 or page_table.shape[0] != n_seqs:
+        raise ValueError("page_table must be [n_seqs, pages]")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
+        raise ValueError("lse must be contiguous float32 [n_q, n_q_heads]")
+    n_new, rows = 0, [None, None, 0, 0, 0, 0, 0]
+    starts = [None, None]
+    if k_new is not None and k_new.shape[0] > 0:
+        if v_new is None or k_new.shape != v_new.shape or k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16 or \
+                tuple(k_new.shape[1:]) != (pool.n_kv_heads, pool.head_dim) or new_start is None or new_len is None:
+            raise ValueError("k_new and v_new must be bfloat16 [rows, n_kv_heads, head_dim], with new_start and new_len")
+        (pk, kt, kh), (pv, vt, vh) = _rows(k_new, "k_new"), _rows(v_new, "v_new")
+        rows = [pk, pv, k_new.shape[0], kt, kh, vt, vh]
+        starts = [_int32(new_start, "new_start", n_seqs), _int32(new_len, "new_len", n_seqs)]
+    pq, qt, qh = _rows(q, "q")
+    po, ot, oh = _rows(out, "out")
+    _check(_load().squat_chunk_attention(
+        pq, q.shape[0], q.shape[1], qt, qh, pool.address, n_seqs, _int32(q_start, "q_start", n_seqs + 1), _int32(cached_len, "cached_len", n_seqs),
+        _int32(page_table, "page_table", page_table.numel()), page_table.shape[1], *rows, *starts, max_q, 1 if causal else 0, softmax_scale,
+        po, ot, oh, None if lse is None else _dev(lse, "lse"), _dev(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), _stream(stream)), "squat_chunk_attention")
 
 
 def squat_get_device_status(clear: bool = True, stream=None) -> int:

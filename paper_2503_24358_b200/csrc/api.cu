@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "squat_internal.cuh"
+#include "chunk_attention.cuh"
 
 namespace {
 
@@ -625,6 +626,213 @@ int squat_decode_attention_pre_rope(const void *q, int q_dtype, int batch, int n
                                  v_scales, v_zeros, n_tokens, cache_stride_b, cache_stride_h, bits, group_size, k_res, v_res,
                                  res_dtype, n_res, softmax_scale, out, workspace, workspace_bytes, rope_table,
                                  (table_positions + 31) / 32, first_pos, 0, stream);
+}
+
+int squat_rope_plan_fill(double base, int head_dim, const int *sections, int n_axes, squat_rope_plan *plan)
+{
+    if (!plan || !sections || n_axes < 1 || n_axes > SQUAT_ROPE_MAX_AXES || !(base > 1.0) || !std::isfinite(base)) return SQUAT_ERR_INVALID_ARG;
+    if (head_dim != D) return SQUAT_ERR_UNSUPPORTED;
+    long long n = 0;
+    for (int a = 0; a < n_axes; ++a) {
+        if (sections[a] < 0) return SQUAT_ERR_INVALID_ARG;
+        n += sections[a];
+    }
+    if (n < 8 || n > D / 2 || n % 8) return SQUAT_ERR_SHAPE;
+    memset(plan, 0, sizeof(*plan));
+    plan->n_pairs = (int)n;
+    plan->n_axes = n_axes;
+    // theta / 2 pi < 0.16 of a turn, so 2^64 of it fits; an 80-bit long double holds it to the last of the 64 bits
+    const long double turns = 18446744073709551616.0L / (2.0L * 3.14159265358979323846264338327950288L);
+    for (int a = 0, i = 0; a < n_axes; ++a)
+        for (int j = 0; j < sections[a]; ++j, ++i) {
+            plan->axis[i] = (unsigned char)a;
+            plan->turn[i] = (unsigned long long)std::floor(turns * std::pow((long double)base, -(long double)i / (long double)n) + 0.5L);
+        }
+    return SQUAT_OK;
+}
+
+int squat_rope_apply(const squat_rope_plan *plan, const void *positions, int positions64, long long axis_stride, int n_tokens,
+                     int head_dim, int dtype, int inverse,
+                     const void *q, int n_q_heads, long long q_stride_t, long long q_stride_h,
+                     void *q_out, long long q_out_stride_t, long long q_out_stride_h,
+                     const void *k, int n_k_heads, long long k_stride_t, long long k_stride_h,
+                     void *k_out, long long k_out_stride_t, long long k_out_stride_h, void *stream)
+{
+    if (!plan || !valid_dtype(dtype) || (positions64 != 0 && positions64 != 1) || (inverse != 0 && inverse != 1) || n_tokens < 0 ||
+        n_q_heads < 0 || n_k_heads < 0 || axis_stride < 0)
+        return SQUAT_ERR_INVALID_ARG;
+    if (head_dim != D) return SQUAT_ERR_UNSUPPORTED;
+    if (plan->n_pairs < 8 || plan->n_pairs > D / 2 || plan->n_pairs % 8 || plan->n_axes < 1 || plan->n_axes > SQUAT_ROPE_MAX_AXES) return SQUAT_ERR_INVALID_ARG;
+    for (int i = 0; i < plan->n_pairs; ++i)
+        if (plan->axis[i] >= plan->n_axes) return SQUAT_ERR_INVALID_ARG;
+    const void *const x[2] = {n_q_heads > 0 ? q : nullptr, n_k_heads > 0 ? k : nullptr};
+    void *const y[2] = {n_q_heads > 0 ? q_out : nullptr, n_k_heads > 0 ? k_out : nullptr};
+    const int heads[2] = {n_q_heads, n_k_heads};
+    const long long strides[2][4] = {{q_stride_t, q_stride_h, q_out_stride_t, q_out_stride_h}, {k_stride_t, k_stride_h, k_out_stride_t, k_out_stride_h}};
+    const long long vec = 16 / (long long)elem_size(dtype);
+    if (n_tokens == 0 || n_q_heads + n_k_heads == 0) return SQUAT_OK;
+    if (!positions || (reinterpret_cast<uintptr_t>(positions) & (positions64 ? 7u : 3u))) return SQUAT_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i) {
+        if (heads[i] == 0) continue;
+        if (!x[i] || !y[i] || !aligned16(x[i]) || !aligned16(y[i])) return SQUAT_ERR_INVALID_ARG;
+        for (int j = 0; j < 4; ++j)
+            if (strides[i][j] < 0 || strides[i][j] % vec) return SQUAT_ERR_INVALID_ARG;
+        // no two output rows in one place, and rows that are written in place stay where they are read
+        if ((n_tokens > 1 && strides[i][2] < D) || (heads[i] > 1 && strides[i][3] < D)) return SQUAT_ERR_INVALID_ARG;
+        if (x[i] == y[i] && ((n_tokens > 1 && strides[i][0] != strides[i][2]) || (heads[i] > 1 && strides[i][1] != strides[i][3]))) return SQUAT_ERR_INVALID_ARG;
+    }
+    return squat_launch_rope(plan, positions, positions64, axis_stride, n_tokens, dtype, inverse, x, y, heads, strides, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+int check_pool(const squat_page_pool *p)
+{
+    if (!p || p->n_pages < 0 || p->page_tokens <= 0 || p->n_kv_heads <= 0 || p->page_stride < 0 || p->head_stride < 0 || (p->meta16 != 0 && p->meta16 != 1))
+        return SQUAT_ERR_INVALID_ARG;
+    if (p->head_dim != D) return SQUAT_ERR_UNSUPPORTED;
+    if (p->bits != 2 && p->bits != 4) return SQUAT_ERR_UNSUPPORTED;
+    if (p->group_size != 32 && p->group_size != 64 && p->group_size != 128) return SQUAT_ERR_UNSUPPORTED;
+    if (p->page_tokens % p->group_size || p->page_stride % p->group_size || p->head_stride % p->group_size) return SQUAT_ERR_SHAPE;
+    if ((long long)p->n_pages * p->page_tokens > 0x7fffffffLL || p->n_kv_heads > 65535) return SQUAT_ERR_UNSUPPORTED;      // a slot is an int
+    if ((p->n_kv_heads > 1 && p->head_stride < p->page_tokens) || (p->n_pages > 1 && p->page_stride < p->page_tokens)) return SQUAT_ERR_INVALID_ARG;
+    if (p->n_pages > 0 && (!p->k_codes || !p->k_scales || !p->k_zeros || !p->v_codes || !p->v_scales || !p->v_zeros)) return SQUAT_ERR_INVALID_ARG;
+    if (!aligned16(p->k_codes) || !aligned16(p->k_scales) || !aligned16(p->k_zeros) || !aligned16(p->v_codes) || !aligned16(p->v_scales) || !aligned16(p->v_zeros))
+        return SQUAT_ERR_INVALID_ARG;
+    return SQUAT_OK;
+}
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Rows [n_tokens, heads, d] that a call reads (x) or writes (y).
+int check_rows(const void *x, long long stride_t, long long stride_h, int n_tokens, int heads, int dtype, bool written)
+{
+    const long long vec = 16 / (long long)elem_size(dtype);
+    if (!aligned16(x) || stride_t < 0 || stride_h < 0 || stride_t % vec || stride_h % vec) return SQUAT_ERR_INVALID_ARG;
+    if (written && ((n_tokens > 1 && stride_t < D) || (heads > 1 && stride_h < D))) return SQUAT_ERR_INVALID_ARG;
+    return SQUAT_OK;
+}
+
+struct PagesWriteLayout {
+    size_t codes, scales, zeros, total;
+};
+PagesWriteLayout pages_write_layout(const squat_page_pool *p, int n_tokens)
+{
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    const size_t toks = (size_t)n_tokens * p->n_kv_heads, meta = up(toks / p->group_size * D * (p->meta16 ? 2 : 4));
+    PagesWriteLayout l;
+    l.codes = 0;
+    l.scales = up(toks * D * p->bits / 8);
+    l.zeros = l.scales + meta;
+    l.total = l.zeros + meta;
+    return l;
+}
+}  // namespace
+
+size_t squat_pages_write_workspace_bytes(const squat_page_pool *pool, int n_tokens)
+{
+    if (check_pool(pool) != SQUAT_OK || n_tokens < 0) return 0;
+    return pages_write_layout(pool, n_tokens).total;
+}
+
+int squat_pages_write(const squat_subspace *s, const squat_page_pool *pool, const int *slots, int n_tokens, int dtype,
+                      const void *k, long long k_stride_t, long long k_stride_h, const void *v, long long v_stride_t,
+                      long long v_stride_h, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_pool(pool);
+    if (rc != SQUAT_OK) return rc;
+    if (!valid_dtype(dtype) || n_tokens < 0) return SQUAT_ERR_INVALID_ARG;
+    if (n_tokens % pool->group_size) return SQUAT_ERR_SHAPE;
+    if (s && !on_handle_device(s)) return SQUAT_ERR_INVALID_ARG;
+    if (s && k && s->n_kv_heads != pool->n_kv_heads) return SQUAT_ERR_SHAPE;
+    if (k && (rc = check_rows(k, k_stride_t, k_stride_h, n_tokens, pool->n_kv_heads, dtype, false)) != SQUAT_OK) return rc;
+    if (v && (rc = check_rows(v, v_stride_t, v_stride_h, n_tokens, pool->n_kv_heads, dtype, false)) != SQUAT_OK) return rc;
+    if (n_tokens == 0 || (!k && !v)) return SQUAT_OK;
+    if (!slots || !aligned4(slots)) return SQUAT_ERR_INVALID_ARG;
+    unsigned *status = squat_status_word();
+    if (!status) return SQUAT_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int n_groups = n_tokens / pool->group_size;
+    if (s && k) {
+        const PagesWriteLayout l = pages_write_layout(pool, n_tokens);
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < l.total || k_stride_t < D) return SQUAT_ERR_INVALID_ARG;
+        char *w = static_cast<char *>(workspace);
+        rc = quantize_keys_impl(s, k, dtype, 1, pool->n_kv_heads, n_tokens, D, 0, k_stride_h, k_stride_t, pool->bits, pool->group_size,
+                                reinterpret_cast<unsigned char *>(w + l.codes), w + l.scales, w + l.zeros, 0, n_tokens, pool->meta16, stream);
+        if (rc != SQUAT_OK) return rc;
+        rc = squat_launch_pages_place(pool, slots, n_groups, w + l.codes, w + l.scales, w + l.zeros, status, st);
+        if (rc != SQUAT_OK) return rc;
+        k = nullptr;
+    }
+    const void *const x[2] = {k, v};
+    void *const y[2] = {nullptr, nullptr};
+    const long long strides[2][2] = {{k_stride_t, k_stride_h}, {v_stride_t, v_stride_h}};
+    return squat_launch_pages(true, pool, slots, n_groups, dtype, x, y, strides, status, st);
+}
+
+int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens, int out_dtype,
+                     void *k_out, long long k_stride_t, long long k_stride_h,
+                     void *v_out, long long v_stride_t, long long v_stride_h, void *stream)
+{
+    int rc = check_pool(pool);
+    if (rc != SQUAT_OK) return rc;
+    if (!valid_dtype(out_dtype) || n_tokens < 0) return SQUAT_ERR_INVALID_ARG;
+    if (n_tokens % pool->group_size) return SQUAT_ERR_SHAPE;
+    if (k_out && (rc = check_rows(k_out, k_stride_t, k_stride_h, n_tokens, pool->n_kv_heads, out_dtype, true)) != SQUAT_OK) return rc;
+    if (v_out && (rc = check_rows(v_out, v_stride_t, v_stride_h, n_tokens, pool->n_kv_heads, out_dtype, true)) != SQUAT_OK) return rc;
+    if (n_tokens == 0 || (!k_out && !v_out)) return SQUAT_OK;
+    if (!slots || !aligned4(slots)) return SQUAT_ERR_INVALID_ARG;
+    unsigned *status = squat_status_word();
+    if (!status) return SQUAT_ERR_CUDA;
+    const void *const x[2] = {nullptr, nullptr};
+    void *const y[2] = {k_out, v_out};
+    const long long strides[2][2] = {{k_stride_t, k_stride_h}, {v_stride_t, v_stride_h}};
+    return squat_launch_pages(false, pool, slots, n_tokens / pool->group_size, out_dtype, x, y, strides, status, static_cast<cudaStream_t>(stream));
+}
+
+size_t squat_chunk_attention_workspace_bytes(int n_q, int n_q_heads, int n_kv_heads, int max_q)
+{
+    if (n_q < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || max_q < 0) return 0;
+    return (squat_chunk_workspace_floats(n_q, n_q_heads, n_kv_heads, max_q) * sizeof(float) + 255) / 256 * 256;
+}
+
+int squat_chunk_attention(const void *q, int n_q, int n_q_heads, long long q_stride_t, long long q_stride_h,
+                          const squat_page_pool *pool, int n_seqs, const int *q_start, const int *cached_len,
+                          const int *page_table, int table_stride, const void *k_new, const void *v_new, int n_new,
+                          long long k_new_stride_t, long long k_new_stride_h, long long v_new_stride_t, long long v_new_stride_h,
+                          const int *new_start, const int *new_len, int max_q, int causal, float softmax_scale,
+                          void *out, long long out_stride_t, long long out_stride_h, float *lse,
+                          void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_pool(pool);
+    if (rc != SQUAT_OK) return rc;
+    if (n_q < 0 || n_q_heads <= 0 || n_seqs < 0 || table_stride < 0 || n_new < 0 || max_q < 0 || (causal != 0 && causal != 1)) return SQUAT_ERR_INVALID_ARG;
+    if (!(softmax_scale >= 0.0f) || !std::isfinite(softmax_scale)) return SQUAT_ERR_INVALID_ARG;
+    if (n_q_heads % pool->n_kv_heads) return SQUAT_ERR_SHAPE;
+    if ((long long)n_q * n_q_heads > 0x7fffffffLL) return SQUAT_ERR_UNSUPPORTED;
+    if ((rc = check_rows(q, q_stride_t, q_stride_h, n_q, n_q_heads, SQUAT_BF16, false)) != SQUAT_OK) return rc;
+    if ((rc = check_rows(out, out_stride_t, out_stride_h, n_q, n_q_heads, SQUAT_BF16, true)) != SQUAT_OK) return rc;
+    if (n_q == 0 || n_seqs == 0) return SQUAT_OK;
+    if (!q || !out || !q_start || !cached_len || !aligned4(q_start) || !aligned4(cached_len) || !aligned4(page_table) || !aligned4(lse)) return SQUAT_ERR_INVALID_ARG;
+    if (table_stride > 0 && pool->n_pages > 0 && !page_table) return SQUAT_ERR_INVALID_ARG;
+    if (n_new > 0) {
+        if (!k_new || !v_new || !new_start || !new_len || !aligned4(new_start) || !aligned4(new_len)) return SQUAT_ERR_INVALID_ARG;
+        if ((rc = check_rows(k_new, k_new_stride_t, k_new_stride_h, n_new, pool->n_kv_heads, SQUAT_BF16, false)) != SQUAT_OK) return rc;
+        if ((rc = check_rows(v_new, v_new_stride_t, v_new_stride_h, n_new, pool->n_kv_heads, SQUAT_BF16, false)) != SQUAT_OK) return rc;
+    }
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < squat_chunk_attention_workspace_bytes(n_q, n_q_heads, pool->n_kv_heads, max_q))
+        return SQUAT_ERR_INVALID_ARG;
+    ChunkParams p = {};
+    p.q = static_cast<const __nv_bfloat16 *>(q);
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.lse = lse;
+    p.qt = q_stride_t; p.qh = q_stride_h; p.ot = out_stride_t; p.oh = out_stride_h;
+    p.n_q = n_q; p.Hq = n_q_heads; p.n_seqs = n_seqs; p.n_new = n_new; p.causal = causal;
+    p.table_stride = page_table ? table_stride : 0;
+    p.q_start = q_start; p.cached_len = cached_len; p.page_table = page_table; p.new_start = new_start; p.new_len = new_len;
+    p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
+    p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
+    p.knt = k_new_stride_t; p.knh = k_new_stride_h; p.vnt = v_new_stride_t; p.vnh = v_new_stride_h;
+    p.scale_log2 = (softmax_scale != 0.0f ? softmax_scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+    return squat_launch_chunk_attention(p, pool, static_cast<float *>(workspace), max_q, static_cast<cudaStream_t>(stream));
 }
 
 #ifdef SQUAT_CHECKED

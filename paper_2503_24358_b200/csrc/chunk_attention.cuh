@@ -1,0 +1,154 @@
+// Attention of new tokens over a paged cache: parameters, and how the work is dealt to CTAs (chunk_attention.cu).
+//
+// An item is (sequence, KV head, R rows), a row being a query of one of the KV head's query heads: row r of a sequence is query
+// r / qpk of head h qpk + r mod qpk.  Its work is tiles of 128 tokens: the sequence's cached tokens, then as many of its
+// rows in full precision as the item's last query sees.  All items' tiles stand in one line, and CTA c takes tiles [c per, (c + 1) per)
+// of it, whatever sequences they belong to: a long sequence among short ones, or a single one, is spread over the GPU
+// without the host knowing a length.  An item that begins and ends within a CTA is finished there; of one that crosses a border,
+// every CTA leaves (sum, maximum, denominator) in the workspace and chunk_combine_kernel adds them up.  A CTA has at most two such
+// parts: of the item that it begins in the middle of (slot 2 c), and of the one it does not finish (slot 2 c + 1).
+#pragma once
+#include "pages.cuh"
+
+constexpr int CHUNK_TILE = 128;                      // tokens
+
+struct ChunkParams {
+    const __nv_bfloat16 *q;
+    __nv_bfloat16 *out;
+    float *lse;
+    long long qt, qh, ot, oh;                        // element strides
+    PagePool pool;
+    int G;
+    int n_q, Hq, H, qpk, n_seqs, table_stride, n_new, causal;
+    const int *q_start, *cached_len, *page_table, *new_start, *new_len;
+    const __nv_bfloat16 *k_new, *v_new;
+    long long knt, knh, vnt, vnh;
+    float scale_log2;                                // softmax scale / ln 2
+    int min_rows, max_rows;                          // the kernel's sequences: those with so many rows
+    int n_cta, min_tiles;                            // CTAs that share the work, and the least that one takes
+    float *part, *ml;                                // [2 n_cta][R][D], [2 n_cta][R][2]
+    unsigned *status;
+};
+
+struct ChunkSeq {
+    int nq, q0, cached, nk, k0;
+};
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams &p, int i)
+{
+    ChunkSeq s;
+    const int a = __ldg(p.q_start + i), b = __ldg(p.q_start + i + 1), c = __ldg(p.cached_len + i);
+    const int k0 = p.n_new > 0 ? __ldg(p.new_start + i) : 0, nk = p.n_new > 0 ? __ldg(p.new_len + i) : 0;
+    s.q0 = min(max(a, 0), p.n_q);
+    s.nq = max(min(b, p.n_q) - s.q0, 0);
+    const long long room = p.pool.n_pages > 0 ? (long long)p.table_stride * p.pool.page_tokens : 0;
+    s.cached = (int)min((long long)max(c, 0), room);
+    s.cached -= s.cached % p.G;
+    s.k0 = min(max(k0, 0), p.n_new);
+    s.nk = min(max(nk, 0), p.n_new - s.k0);
+    if (s.q0 != a || s.q0 + s.nq != b || s.cached != c || s.k0 != k0 || s.nk != nk) atomicOr(p.status, SQUAT_FLAG_PAGES);
+    const long long rows = (long long)s.nq * p.qpk;
+    if (rows < p.min_rows || rows > p.max_rows) s.nq = 0;
+    return s;
+}
+// rows in full precision that query j sees
+__device__ __forceinline__ int chunk_sees(const ChunkParams &p, const ChunkSeq &s, int j)
+{
+    return p.causal ? min(max(s.nk - s.nq + j + 1, 0), s.nk) : s.nk;
+}
+template <int R>
+__device__ __forceinline__ int chunk_row_tiles(const ChunkParams &p, const ChunkSeq &s) { return (int)(((long long)s.nq * p.qpk + R - 1) / R); }
+// tiles of the sequence's rows qt R .. of one head; at least one, which writes the zeros of rows that see nothing
+template <int R>
+__device__ __forceinline__ int chunk_tiles(const ChunkParams &p, const ChunkSeq &s, int qt)
+{
+    const int last = (int)(min((long long)s.nq * p.qpk, (long long)(qt + 1) * R) - 1) / p.qpk;
+    const int n = (s.cached + CHUNK_TILE - 1) / CHUNK_TILE + (chunk_sees(p, s, last) + CHUNK_TILE - 1) / CHUNK_TILE;
+    return max(n, 1);
+}
+template <int R>
+__device__ __forceinline__ long long chunk_head_tiles(const ChunkParams &p, const ChunkSeq &s)
+{
+    const int n = chunk_row_tiles<R>(p, s);
+    long long sum = 0;
+    for (int qt = 0; qt < n; ++qt) sum += chunk_tiles<R>(p, s, qt);
+    return sum;
+}
+
+// A place in the line of tiles: item and tile within it.
+struct ChunkPlace {
+    int seq, h, qt, tile;
+};
+struct ChunkShared {
+    long long sums[33];
+    ChunkPlace found;
+};
+
+// All threads of the CTA (a multiple of 32, at most 1024) call this.  per: tiles per CTA, total: of all sequences.
+template <int R>
+__device__ __forceinline__ void chunk_share(const ChunkParams &p, ChunkShared &sm, long long &per, long long &total)
+{
+    long long mine = 0;
+    for (int i = threadIdx.x; i < p.n_seqs; i += blockDim.x) mine += chunk_head_tiles<R>(p, chunk_seq(p, i)) * p.H;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if ((threadIdx.x & 31) == 0) sm.sums[threadIdx.x >> 5] = mine;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < (int)blockDim.x >> 5; ++w) total += sm.sums[w];
+    per = max((total + p.n_cta - 1) / p.n_cta, (long long)p.min_tiles);
+    __syncthreads();
+}
+// The item that holds tile `at` of the line (at < total), for all threads.
+template <int R>
+__device__ __forceinline__ ChunkPlace chunk_locate(const ChunkParams &p, ChunkShared &sm, long long at)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    long long before = 0;
+    for (int base = 0; base < p.n_seqs; base += blockDim.x) {
+        const int i = base + threadIdx.x;
+        ChunkSeq s = {};
+        long long head = 0, sum;
+        if (i < p.n_seqs) {
+            s = chunk_seq(p, i);
+            head = chunk_head_tiles<R>(p, s);
+        }
+        sum = head * p.H;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 31) sm.sums[warp] = sum;
+        __syncthreads();
+        long long end = before + sum;
+        for (int w = 0; w < warp; ++w) end += sm.sums[w];
+        const long long begin = end - head * p.H;
+        if (head > 0 && at >= begin && at < end) {
+            long long rest = (at - begin) % head;
+            int qt = 0;
+            for (int n; rest >= (n = chunk_tiles<R>(p, s, qt)); ++qt) rest -= n;
+            sm.found = {i, (int)((at - begin) / head), qt, (int)rest};
+        }
+        for (int w = 0; w < warps; ++w) before += sm.sums[w];
+        __syncthreads();
+        if (before > at) break;
+    }
+    return sm.found;
+}
+// To the next item.
+template <int R>
+__device__ __forceinline__ void chunk_next(const ChunkParams &p, ChunkPlace &w, ChunkSeq &s)
+{
+    w.tile = 0;
+    if (++w.qt < chunk_row_tiles<R>(p, s)) return;
+    w.qt = 0;
+    if (++w.h < p.H) return;
+    w.h = 0;
+    do {
+        if (++w.seq >= p.n_seqs) return;
+        s = chunk_seq(p, w.seq);
+    } while (s.nq == 0);
+}
+
+constexpr int CHUNK_ROWS = 16;                       // rows of an item in the kernel for few rows
+int squat_launch_chunk_rows(const ChunkParams &p, int bits, int meta16, cudaStream_t st);

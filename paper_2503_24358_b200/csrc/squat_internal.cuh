@@ -143,6 +143,17 @@ int squat_launch_dequant(int kind, const unsigned char *codes, const void *scale
                          int batch, int H, int T, int d, int bits, int G, long long isb, long long ish,
                          void *out, int out_dtype, int meta16, cudaStream_t st);
 
+struct ChunkParams;                          // chunk_attention.cuh
+int squat_launch_rope(const squat_rope_plan *plan, const void *positions, int positions64, long long axis_stride, int n_tokens,
+                      int dtype, int inverse, const void *const (&x)[2], void *const (&y)[2], const int (&heads)[2],
+                      const long long (&strides)[2][4], cudaStream_t st);
+int squat_launch_pages(bool write, const squat_page_pool *pool, const int *slots, int n_groups, int dtype,
+                       const void *const (&x)[2], void *const (&y)[2], const long long (&strides)[2][2], unsigned *status, cudaStream_t st);
+int squat_launch_pages_place(const squat_page_pool *pool, const int *slots, int n_groups, const void *codes, const void *scales,
+                             const void *zeros, unsigned *status, cudaStream_t st);
+size_t squat_chunk_workspace_floats(int n_q, int n_q_heads, int n_kv_heads, int max_q);
+int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, float *workspace, int max_q, cudaStream_t st);
+
 // ---- the bounds-checked build ----------------------------------------------------------
 // Compiled with -DSQUAT_CHECKED (build.py --checked -> libsquat_checked.so) the key and value kernels test every
 // global, shared-memory and tensor-memory address they form (and the shared-memory windows of the matrix descriptors
