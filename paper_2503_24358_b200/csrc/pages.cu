@@ -4,27 +4,37 @@
 //
 // Delta is a product of binary32 numbers: its last bit may differ from the rounded quotient that the quantizers of contiguous
 // caches store.  Codes are decided by the stored grid, so this is no error of theirs.
-// over G tokens per channel (keys) or G channels per token (values).  A CTA takes one group of tokens of one head: G tokens
-// are G rows of 256 or 512 contiguous bytes, and 16 threads hold a row, eight channels each, four rows to a thread.  So both
-// reductions are short: keys over the rows (a thread's four, the two halves of a warp, the warps), values over neighbouring lanes.
+// over G tokens per channel (keys) or G channels per token (values).
+//
+// Keys: a group is G rows of 256 or 512 contiguous bytes.  16 threads hold a row, eight channels each, eight rows to a thread; the
+// minima of a thread's rows (bf16: of channel pairs, packed), of the halves of a warp, then of the group's 2 to 8 warps.  Values: a
+// thread holds 32 channels of a token, as the quantizer of contiguous caches does; groups of 64 and 128 are 2 and 4 lanes.
 //
 // Decisions.  t is bracketed by (x - z) r (1 +- 2^-20), r the hardware reciprocal of Delta (1 ulp); adding 1.5 * 2^23 rounds both
-// ends to integers, ties to even, and where they agree that integer is the code.  Where they do not (structural with bf16
-// data), values take the IEEE binary32 sequence that defines them, keys the sign of (x - z) - (k + 1/2) Delta in float64: what
-// real arithmetic on the stored grid decides.
+// ends to integers, ties to even, and where they agree that integer is the code.  Both ends are packed by shifted adds; the ends
+// differ by one level at most, so the difference of the packed words has a bit for every element that is open (structural with
+// bf16 data).  Those are decided one by one (patch).
 //
 // Bound: HBM (x is read once, codes and metadata are written once; a group's codes are one contiguous span of its page).
+#include <type_traits>
 #include "pages.cuh"
 
 namespace {
 
 constexpr int D = SQUAT_D;
 constexpr float kMagic = 12582912.0f;   // 1.5 * 2^23
-constexpr int ROWS = 4;                 // rows of a group per thread
+constexpr int READ_THREADS = 256;
+constexpr int ROWS = 8;                 // rows of a group per thread
+// groups and threads of a CTA: 64 tokens and 128 threads, or (G = 128) twice as many
+template <int G>
+struct Cta {
+    static constexpr int TOKENS = G < 64 ? 64 : G, GROUPS = TOKENS / G, THREADS = 2 * TOKENS;
+};
 
 struct PagesParams {
     PagePool pool;
     const int *slots;
+    int n_groups;
     int first;                          // 0: keys and (blockIdx.z = 1) values, 1: values only
     const void *x[2];                   // keys, values
     long long xt[2], xh[2];
@@ -33,86 +43,150 @@ struct PagesParams {
 };
 
 // A group's grid as it is stored, and what decides by it.
-struct Grid {
-    float zero, delta, ra, rb;
+template <int BITS, bool M16>
+__device__ __forceinline__ void grid_of(float m, float Mx, float &zero, float &delta)
+{
+    constexpr float invL = 1.0f / float((1 << BITS) - 1);
+    delta = __fmul_rn(__fsub_rn(Mx, m), invL);
+    zero = m;
+    if (M16) {
+        delta = __half2float(__float2half_rn(delta));
+        zero = __half2float(__float2half_rn(m));
+    }
+}
+struct Ends {
+    float ra, rb;                       // reciprocal of the scale, a little more and a little less
     bool ok, fast;
 };
-template <int BITS, bool M16>
-__device__ __forceinline__ Grid grid_of(float m, float Mx)
+__device__ __forceinline__ Ends ends_of(float delta)
 {
-    Grid g;
-    constexpr float invL = 1.0f / float((1 << BITS) - 1);
-    g.delta = __fmul_rn(__fsub_rn(Mx, m), invL);
-    g.zero = m;
-    if (M16) {
-        g.delta = __half2float(__float2half_rn(g.delta));
-        g.zero = __half2float(__float2half_rn(m));
-    }
-    return g;
-}
-__device__ __forceinline__ void decide_by(Grid &g)
-{
-    g.ok = g.delta > 0.0f && g.delta < __int_as_float(0x7f800000);
-    g.fast = g.delta > 0x1p-100f && g.delta < 0x1p100f;
+    Ends e;
+    e.ok = delta > 0.0f && delta < __int_as_float(0x7f800000);
+    e.fast = delta > 0x1p-100f && delta < 0x1p100f;
     float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(g.delta));
-    g.ra = __fmul_rn(r, 1.0f + 0x1p-20f);
-    g.rb = __fmul_rn(r, 1.0f - 0x1p-20f);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(delta));
+    e.ra = __fmul_rn(r, 1.0f + 0x1p-20f);
+    e.rb = __fmul_rn(r, 1.0f - 0x1p-20f);
+    return e;
 }
 
-// The code where the bracket leaves it open.
+// A code that the bracket leaves open: `hi`, its upper end, or one less.  The border is k = hi - 1/2, and the sign of (x - z) - k Delta,
+// one fma, says on which side x lies; zero is a tie and goes to the even code.  Where x - z is no float32 number (keys), the
+// remainder too small for the quotient's own rounding (values) or the scale beyond the bracket's range (slow): the division.
 template <int BITS, bool KEY>
-__device__ __noinline__ unsigned exact_code(float x, float zero, float delta)
+__device__ __forceinline__ unsigned decide(float x, float z, float d, unsigned hi, bool slow)
 {
     constexpr float L = float((1 << BITS) - 1);
-    if (!KEY) return (unsigned)(int)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x, zero), delta)), 0.0f), L);
-    const double dl = (double)x - (double)zero;
-    return (unsigned)(int)fmin(fmax(rint(__ddiv_rn(dl, (double)delta)), 0.0), (double)L);
+    const float dl = __fsub_rn(x, z), k = (float)hi - 0.5f, r = __fmaf_rn(-k, d, dl), back = __fsub_rn(x, dl);
+    const bool sure = KEY ? __fadd_rn(__fsub_rn(x, __fadd_rn(dl, back)), __fsub_rn(back, z)) == 0.0f : r == 0.0f || fabsf(r) > k * d * 0x1p-21f;
+    if (sure && !slow) return r > 0.0f || (r == 0.0f && (hi & 1u) == 0) ? hi : hi - 1u;
+    if (KEY) return (unsigned)(int)fmin(fmax(rint(__ddiv_rn((double)x - (double)z, (double)d)), 0.0), (double)L);
+    return (unsigned)(int)fminf(fmaxf(rintf(__fdiv_rn(dl, d)), 0.0f), L);
 }
-
-// Eight codes, packed low bits first.
-template <int BITS, bool KEY, bool M16>
-__device__ __forceinline__ unsigned codes_of(const float (&x)[8], const Grid *g, int g_step)
+template <bool BF16>
+__device__ __forceinline__ float element(const void *src, long long at)
 {
-    constexpr float L = float((1 << BITS) - 1);
-    unsigned word = 0, open = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const Grid &gr = g[i * g_step];
-        const float dl = __fsub_rn(x[i], gr.zero);
-        float ya = __fmaf_rn(dl, gr.ra, kMagic), yb = __fmaf_rn(dl, gr.rb, kMagic);
-        if (M16) {                                  // a rounded zero-point may lie above the minimum
-            ya = fminf(fmaxf(ya, kMagic), kMagic + L);
-            yb = fminf(fmaxf(yb, kMagic), kMagic + L);
-        }
-        if (!gr.fast || ya != yb) open |= 1u << i;
-        word |= gr.ok ? (__float_as_uint(ya) & ((1u << BITS) - 1u)) << (BITS * i) : 0u;
-    }
-    if (open) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const Grid &gr = g[i * g_step];
-            if (!(open >> i & 1) || !gr.ok) continue;
-            word = (word & ~(((1u << BITS) - 1u) << (BITS * i))) | exact_code<BITS, KEY>(x[i], gr.zero, gr.delta) << (BITS * i);
-        }
+    return BF16 ? __uint_as_float((unsigned)__ldg(static_cast<const unsigned short *>(src) + at) << 16) : __ldg(static_cast<const float *>(src) + at);
+}
+// A word of a token's values, one bit of `open` for each open code; out of line, and from memory again (it is in L1), so that the
+// streaming code stays small.
+template <int BITS, bool BF16>
+__device__ __noinline__ unsigned patch_values(unsigned word, unsigned open, const void *src, long long at, float zero, float delta, bool slow)
+{
+    constexpr unsigned FIELD = (1u << BITS) - 1u;
+    while (open) {
+        const int pos = __ffs(open) - 1;
+        open &= open - 1;
+        word = (word & ~(FIELD << pos)) | decide<BITS, false>(element<BF16>(src, at + pos / BITS), zero, delta, word >> pos & FIELD, slow) << pos;
     }
     return word;
 }
 
-template <bool BF16>
-__device__ __forceinline__ void load_row(const void *p, long long at, float (&x)[8])
+// Both ends of N codes (N * BITS <= 32, N even), packed low bits first.  zero2, ra2, rb2: pairs of neighbouring elements', STEP pairs apart
+template <int BITS, int N, int STEP, bool M16>
+__device__ __forceinline__ void pack_ends(const u64 *x2, const u64 *zero2, const u64 *ra2, const u64 *rb2, unsigned &a, unsigned &b)
 {
-    if (BF16) {
-        const uint4 r = ldg128(static_cast<const __nv_bfloat16 *>(p) + at);
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    constexpr float L = float((1 << BITS) - 1);
+    constexpr unsigned K = [] { unsigned k = 0; for (int i = 0; i < N; ++i) k += 0x4B400000u << (BITS * i); return k; }();
+    const u64 magic2 = pack2(kMagic, kMagic);
+    a = b = 0u - K;                     // what the constant upper bits add up to
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = bf16lo_to_f32(w[i]); x[2 * i + 1] = bf16hi_to_f32(w[i]); }
-    } else {
-        const float4 *s = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at);
-        const float4 a = __ldg(s), b = __ldg(s + 1);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    for (int i = 0; i < N / 2; ++i) {
+        const u64 dl = fsub2(x2[i], zero2[i * STEP]);
+        float a0, a1, b0, b1;
+        unpack2(ffma2(dl, ra2[i * STEP], magic2), a0, a1);
+        unpack2(ffma2(dl, rb2[i * STEP], magic2), b0, b1);
+        if (M16) {                      // a rounded zero-point may lie above the minimum
+            a0 = fminf(fmaxf(a0, kMagic), kMagic + L); b0 = fminf(fmaxf(b0, kMagic), kMagic + L);
+            a1 = fminf(fmaxf(a1, kMagic), kMagic + L); b1 = fminf(fmaxf(b1, kMagic), kMagic + L);
+        }
+        a += __float_as_uint(a0) << (BITS * 2 * i);
+        a += __float_as_uint(a1) << (BITS * (2 * i + 1));
+        b += __float_as_uint(b0) << (BITS * 2 * i);
+        b += __float_as_uint(b1) << (BITS * (2 * i + 1));
     }
 }
+template <int BITS, int N>
+constexpr unsigned LOW_BITS = [] { unsigned m = 0; for (int i = 0; i < N; ++i) m |= 1u << (BITS * i); return m; }();
+
+// Eight channels of a row as they were loaded; widened where they are used.
+template <bool BF16>
+struct Row8;
+template <>
+struct Row8<true> {
+    uint4 r;
+    __device__ __forceinline__ void load(const void *p, long long at) { r = ldg128(static_cast<const __nv_bfloat16 *>(p) + at); }
+    __device__ __forceinline__ u64 pair(int i) const
+    {
+        const uint32_t w = i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w;
+        return pack2(bf16lo_to_f32(w), bf16hi_to_f32(w));
+    }
+};
+template <>
+struct Row8<false> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const void *p, long long at)
+    {
+        const float4 *s = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at);
+        a = __ldg(s);
+        b = __ldg(s + 1);
+    }
+    __device__ __forceinline__ u64 pair(int i) const { return i == 0 ? pack2(a.x, a.y) : i == 1 ? pack2(a.z, a.w) : i == 2 ? pack2(b.x, b.y) : pack2(b.z, b.w); }
+};
+// Minimum and maximum of pairs of channels: packed bf16, or two floats.
+template <bool BF16>
+struct MinMax2;
+template <>
+struct MinMax2<true> {
+    unsigned lo, hi;
+    __device__ __forceinline__ void start(const Row8<true> &r, int i) { lo = hi = i == 0 ? r.r.x : i == 1 ? r.r.y : i == 2 ? r.r.z : r.r.w; }
+    __device__ __forceinline__ void join(const MinMax2 &o) { lo = hmin2_nan_bits(lo, o.lo); hi = hmax2_nan_bits(hi, o.hi); }
+    __device__ __forceinline__ MinMax2 other(int lanes) const { return {__shfl_xor_sync(0xffffffffu, lo, lanes), __shfl_xor_sync(0xffffffffu, hi, lanes)}; }
+    __device__ __forceinline__ float2 min2() const { return make_float2(bf16lo_to_f32(lo), bf16hi_to_f32(lo)); }
+    __device__ __forceinline__ float2 max2() const { return make_float2(bf16lo_to_f32(hi), bf16hi_to_f32(hi)); }
+};
+template <>
+struct MinMax2<false> {
+    float2 lo, hi;
+    __device__ __forceinline__ void start(const Row8<false> &r, int i)
+    {
+        float x, y;
+        unpack2(r.pair(i), x, y);
+        lo = hi = make_float2(x, y);
+    }
+    __device__ __forceinline__ void join(const MinMax2 &o)
+    {
+        lo = make_float2(min_nan(lo.x, o.lo.x), min_nan(lo.y, o.lo.y));
+        hi = make_float2(max_nan(hi.x, o.hi.x), max_nan(hi.y, o.hi.y));
+    }
+    __device__ __forceinline__ MinMax2 other(int lanes) const
+    {
+        return {make_float2(__shfl_xor_sync(0xffffffffu, lo.x, lanes), __shfl_xor_sync(0xffffffffu, lo.y, lanes)),
+                make_float2(__shfl_xor_sync(0xffffffffu, hi.x, lanes), __shfl_xor_sync(0xffffffffu, hi.y, lanes))};
+    }
+    __device__ __forceinline__ float2 min2() const { return lo; }
+    __device__ __forceinline__ float2 max2() const { return hi; }
+};
 
 template <bool M16>
 __device__ __forceinline__ void store_meta(void *p, long long i, float v)
@@ -126,119 +200,223 @@ __device__ __forceinline__ float load_meta(const void *p, long long i)
     return M16 ? __half2float(__ldg(static_cast<const __half *>(p) + i)) : __ldg(static_cast<const float *>(p) + i);
 }
 
-// The group's first token in the pool, or -1: padding or (flagged) a slot that is none.
+// A group's first token in the pool, or -1: padding or (flagged) a slot that is none.
 template <int G>
-__device__ __forceinline__ long long group_token(const PagesParams &p, const int *slots, int h)
+__device__ __forceinline__ long long group_token(const PagesParams &p, const int *slots, int group, int h)
 {
-    const int slot = __ldg(slots + blockIdx.x);
+    const int slot = __ldg(slots + group);
     if (slot < 0) return -1;
     if (slot % G != 0 || slot / p.pool.page_tokens >= p.pool.n_pages) {
-        if (threadIdx.x == 0) atomicOr(p.status, SQUAT_FLAG_PAGES);
+        atomicOr(p.status, SQUAT_FLAG_PAGES);
         return -1;
     }
     return token_at_slot(p.pool, slot, h);
 }
 
-// grid (groups, heads, keys / values); 4 G threads: thread t holds channels 8 (t mod 16) .. + 7 of rows t / 16 + (G / 4) i
-template <int G, int BITS, bool BF16, bool M16>
-__global__ void __launch_bounds__(4 * G) pages_write_kernel(PagesParams p)
+// The threads of one of a CTA's groups.  (Barriers by constant numbers: a number in a register reserves all sixteen, and CTAs with
+// sixteen each are few to an SM.)
+template <int GROUPS, int N>
+__device__ __forceinline__ void sync_group(int group)
 {
-    constexpr int WARPS = G / 8, STEP = G / ROWS;
-    __shared__ __align__(16) float lo_sm[WARPS][D], hi_sm[WARPS][D];
-    const int part = p.first + blockIdx.z, h = blockIdx.y, tid = threadIdx.x, c8 = tid & 15, r0 = tid >> 4;
+    if (GROUPS == 1) __syncthreads();
+    else if (group == 0) asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
+    else asm volatile("bar.sync 2, %0;" ::"n"(N) : "memory");
+}
+
+template <int G, int BITS, bool BF16, bool M16>
+__device__ __forceinline__ void write_keys(const PagesParams &p, const void *src, const int *slots)
+{
+    using C = Cta<G>;
+    constexpr int WARPS = G / 16, LANES = G / ROWS;          // of a group; threads of a group that share a channel
+    using word_t = typename std::conditional<BITS == 2, unsigned short, unsigned>::type;         // eight codes
+    __shared__ MinMax2<BF16> ends_sm[C::GROUPS][WARPS][D / 2];
+    __shared__ __align__(16) word_t words_sm[C::TOKENS][16];
+    __shared__ word_t open_sm[ROWS][C::THREADS];
+    __shared__ __align__(16) float2 zero_sm[C::GROUPS][D / 2], delta_sm[C::GROUPS][D / 2];
+    const int h = blockIdx.y, tid = threadIdx.x, c8 = tid & 15, r0 = (tid >> 4) % LANES, mine = tid / (16 * LANES), group = blockIdx.x * C::GROUPS + mine;
+    const long long tok = group < p.n_groups ? group_token<G>(p, slots, group, h) : -1;
+    const long long at = ((long long)group * G + r0) * p.xt[0] + (long long)h * p.xh[0] + 8 * c8;
+    Row8<BF16> x[ROWS];
+    if (tok >= 0) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) x[i].load(src, at + (long long)(LANES * i) * p.xt[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            MinMax2<BF16> e, o;
+            e.start(x[0], c);
+#pragma unroll
+            for (int i = 1; i < ROWS; ++i) {
+                o.start(x[i], c);
+                e.join(o);
+            }
+            e.join(e.other(16));                             // (a warp's rows belong to one group)
+            if ((tid & 16) == 0) ends_sm[mine][(tid >> 5) % WARPS][4 * c8 + c] = e;
+        }
+    }
+    __syncthreads();
+    const int pr = tid % (16 * LANES);                       // a pair of channels' grids
+    if (tok >= 0 && pr < D / 2) {
+        MinMax2<BF16> e = ends_sm[mine][0][pr];
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) e.join(ends_sm[mine][w][pr]);
+        const float2 lo = e.min2(), hi = e.max2();
+        float2 z, d;
+        grid_of<BITS, M16>(lo.x, hi.x, z.x, d.x);
+        grid_of<BITS, M16>(lo.y, hi.y, z.y, d.y);
+        zero_sm[mine][pr] = z;
+        delta_sm[mine][pr] = d;
+        const long long to = tok / G * (D / 2) + pr;
+        if (M16) {
+            static_cast<__half2 *>(p.pool.ks)[to] = __floats2half2_rn(d.x, d.y);
+            static_cast<__half2 *>(p.pool.kz)[to] = __floats2half2_rn(z.x, z.y);
+        } else {
+            static_cast<float2 *>(p.pool.ks)[to] = d;
+            static_cast<float2 *>(p.pool.kz)[to] = z;
+        }
+        const bool none = d.x == 0.0f || d.y == 0.0f, odd = !(d.x < INFINITY && d.y < INFINITY);
+        if (none || odd) atomicOr(p.status, (none ? SQUAT_FLAG_ZERO_RANGE : 0u) | (odd ? SQUAT_FLAG_NONFINITE : 0u));
+    }
+    __syncthreads();
+    if (tok < 0) return;
+    u64 zero2[4], ra2[4], rb2[4];
+    unsigned keep = 0, slow = 0;                             // fields of channels with a grid; bits of those the bracket is not good for
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const float2 z = zero_sm[mine][4 * c8 + c], d = delta_sm[mine][4 * c8 + c];
+        const Ends a = ends_of(d.x), b = ends_of(d.y);
+        zero2[c] = pack2(z.x, z.y);
+        ra2[c] = pack2(a.ra, b.ra);
+        rb2[c] = pack2(a.rb, b.rb);
+        keep |= (a.ok ? ((1u << BITS) - 1u) << (BITS * 2 * c) : 0u) | (b.ok ? ((1u << BITS) - 1u) << (BITS * (2 * c + 1)) : 0u);
+        slow |= (a.fast ? 0u : 1u << (BITS * 2 * c)) | (b.fast ? 0u : 1u << (BITS * (2 * c + 1)));
+    }
+    // words first; the open ones of all rows then in one loop, so that a warp's lanes take theirs at the same time
+    unsigned rows = 0;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        u64 x2[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x2[c] = x[i].pair(c);
+        unsigned word, low;
+        pack_ends<BITS, 8, 1, M16>(x2, zero2, ra2, rb2, word, low);
+        const unsigned open = ((word - low) | slow) & keep & LOW_BITS<BITS, 8>;
+        words_sm[r0 + LANES * i + G * mine][c8] = (word_t)(word & keep);
+        if (open) {
+            rows |= 1u << i;
+            open_sm[i][tid] = (word_t)open;
+        }
+    }
+    if (rows) {
+        unsigned open = 0;
+        int i = 0;
+        while (rows | open) {
+            if (open == 0) {
+                i = __ffs(rows) - 1;
+                rows &= rows - 1;
+                open = open_sm[i][tid];
+            }
+            constexpr unsigned FIELD = (1u << BITS) - 1u;
+            const int pos = __ffs(open) - 1, c = pos / BITS;
+            open &= open - 1;
+            word_t &to = words_sm[r0 + LANES * i + G * mine][c8];
+            const unsigned word = to;
+            to = (word_t)((word & ~(FIELD << pos)) | decide<BITS, true>(element<BF16>(src, at + (long long)(LANES * i) * p.xt[0] + c), (&zero_sm[mine][4 * c8].x)[c], (&delta_sm[mine][4 * c8].x)[c],
+                                                                       word >> pos & FIELD, slow >> pos & 1u) << pos);
+        }
+    }
+    // a warp's rows of step i are two neighbouring tokens; the codes of the group are one span
+    sync_group<C::GROUPS, 16 * LANES>(mine);
+    uint4 *to = reinterpret_cast<uint4 *>(p.pool.kc + tok * (D * BITS / 8));
+#pragma unroll
+    for (int i = 0; i < G * BITS / (16 * LANES); ++i) to[pr + 16 * LANES * i] = reinterpret_cast<const uint4 *>(&words_sm[G * mine][0])[pr + 16 * LANES * i];
+}
+
+// Four lanes a token, two tokens a thread
+template <int G, int BITS, bool BF16, bool M16>
+__device__ __forceinline__ void write_values(const PagesParams &p, const void *src, const int *slots)
+{
+    using C = Cta<G>;
+    constexpr int LANES = G / 32, PER_WORD = 32 / BITS, WORDS = BITS;        // lanes of a group; words of a thread's codes
+    const int h = blockIdx.y, tid = threadIdx.x, span = tid & 3;
+    Row8<BF16> x[2][4];
+    long long tok[2], at[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int t = (tid >> 2) + C::TOKENS / 2 * j;                        // token of the CTA
+        const int group = blockIdx.x * C::GROUPS + t / G;
+        tok[j] = group < p.n_groups ? group_token<G>(p, slots, group, h) : -1;
+        if (tok[j] < 0) continue;
+        tok[j] += t % G;
+        at[j] = ((long long)blockIdx.x * C::TOKENS + t) * p.xt[1] + (long long)h * p.xh[1] + 32 * span;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[j][i].load(src, at[j] + 8 * i);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        if (tok[j] < 0) continue;                            // (all lanes of a warp hold tokens of one group, or of one and a missing one)
+        MinMax2<BF16> e, o;
+        e.start(x[j][0], 0);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) {
+            o.start(x[j][i / 4], i % 4);
+            e.join(o);
+        }
+#pragma unroll
+        for (int l = 1; l < LANES; l <<= 1) e.join(e.other(l));
+        const float2 lo = e.min2(), hi = e.max2();
+        float zero, delta;
+        grid_of<BITS, M16>(min_nan(lo.x, lo.y), max_nan(hi.x, hi.y), zero, delta);
+        const Ends r = ends_of(delta);
+        const u64 zero2 = pack2(zero, zero), ra2 = pack2(r.ra, r.ra), rb2 = pack2(r.rb, r.rb);
+        unsigned words[WORDS];
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            u64 x2[PER_WORD / 2];
+#pragma unroll
+            for (int i = 0; i < PER_WORD / 2; ++i) x2[i] = x[j][(w * PER_WORD / 2 + i) / 4].pair((w * PER_WORD / 2 + i) % 4);
+            unsigned word, low;
+            pack_ends<BITS, PER_WORD, 0, M16>(x2, &zero2, &ra2, &rb2, word, low);
+            unsigned open = r.fast ? word - low : LOW_BITS<BITS, PER_WORD>;
+            if (open && r.ok) word = patch_values<BITS, BF16>(word, open, src, at[j] + w * PER_WORD, zero, delta, !r.fast);
+            words[w] = r.ok ? word : 0u;
+        }
+        unsigned char *to = p.pool.vc + tok[j] * (D * BITS / 8) + span * (4 * BITS);
+        if (BITS == 2) *reinterpret_cast<uint2 *>(to) = make_uint2(words[0], words[1]);
+        else *reinterpret_cast<uint4 *>(to) = make_uint4(words[0], words[1], words[BITS - 2], words[BITS - 1]);
+        if (span % LANES == 0) {
+            const long long m = tok[j] * (D / G) + span / LANES;
+            store_meta<M16>(p.pool.vs, m, delta);
+            store_meta<M16>(p.pool.vz, m, zero);
+            if (!r.ok) atomicOr(p.status, delta == 0.0f ? SQUAT_FLAG_ZERO_RANGE : SQUAT_FLAG_NONFINITE);
+        }
+    }
+}
+
+// grid (CTAs' tokens, heads, keys / values)
+template <int G, int BITS, bool BF16, bool M16>
+__global__ void __launch_bounds__(Cta<G>::THREADS, (BF16 ? 6 : 4) * 128 / Cta<G>::THREADS) pages_write_kernel(PagesParams p)
+{
+    const int part = p.first + blockIdx.z;
     const void *src = p.x[part];
     const int *slots = p.slots;
     grid_wait(src, slots);
-    const long long tok = group_token<G>(p, slots, h);
-    if (tok < 0) return;
-    float x[ROWS][8];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i)
-        load_row<BF16>(src, ((long long)blockIdx.x * G + r0 + STEP * i) * p.xt[part] + (long long)h * p.xh[part] + 8 * c8, x[i]);
-    unsigned char *codes = (part == 0 ? p.pool.kc : p.pool.vc) + (tok + r0) * (D * BITS / 8) + c8 * BITS;
-    unsigned words[ROWS], flags = 0;
-    if (part == 0) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            float m = min_nan(min_nan(x[0][c], x[1][c]), min_nan(x[2][c], x[3][c])), Mx = max_nan(max_nan(x[0][c], x[1][c]), max_nan(x[2][c], x[3][c]));
-            m = min_nan(m, __shfl_xor_sync(0xffffffffu, m, 16));
-            Mx = max_nan(Mx, __shfl_xor_sync(0xffffffffu, Mx, 16));
-            if ((tid & 16) == 0) {
-                lo_sm[tid >> 5][8 * c8 + c] = m;
-                hi_sm[tid >> 5][8 * c8 + c] = Mx;
-            }
-        }
-        __syncthreads();
-        if (tid < D) {                                   // a channel's grid
-            float m = lo_sm[0][tid], Mx = hi_sm[0][tid];
-#pragma unroll
-            for (int w = 1; w < WARPS; ++w) {
-                m = min_nan(m, lo_sm[w][tid]);
-                Mx = max_nan(Mx, hi_sm[w][tid]);
-            }
-            const Grid g = grid_of<BITS, M16>(m, Mx);
-            lo_sm[0][tid] = g.zero;
-            hi_sm[0][tid] = g.delta;
-            const long long at = tok / G * D + tid;
-            store_meta<M16>(p.pool.ks, at, g.delta);
-            store_meta<M16>(p.pool.kz, at, g.zero);
-            if (!(g.delta > 0.0f && g.delta < __int_as_float(0x7f800000))) flags = g.delta == 0.0f ? SQUAT_FLAG_ZERO_RANGE : SQUAT_FLAG_NONFINITE;
-        }
-        __syncthreads();
-        Grid g[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            g[c].zero = lo_sm[0][8 * c8 + c];
-            g[c].delta = hi_sm[0][8 * c8 + c];
-            decide_by(g[c]);
-        }
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) words[i] = codes_of<BITS, true, M16>(x[i], g, 1);
-    } else {
-        constexpr int LANES = G / 8;                     // of a group
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            float m = x[i][0], Mx = x[i][0];
-#pragma unroll
-            for (int c = 1; c < 8; ++c) { m = min_nan(m, x[i][c]); Mx = max_nan(Mx, x[i][c]); }
-#pragma unroll
-            for (int o = 1; o < LANES; o <<= 1) {
-                m = min_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-                Mx = max_nan(Mx, __shfl_xor_sync(0xffffffffu, Mx, o));
-            }
-            Grid g = grid_of<BITS, M16>(m, Mx);
-            decide_by(g);
-            words[i] = codes_of<BITS, false, M16>(x[i], &g, 0);
-            if (c8 % LANES == 0) {
-                const long long at = (tok + r0 + STEP * i) * (D / G) + c8 / LANES;
-                store_meta<M16>(p.pool.vs, at, g.delta);
-                store_meta<M16>(p.pool.vz, at, g.zero);
-                if (!g.ok) flags |= g.delta == 0.0f ? SQUAT_FLAG_ZERO_RANGE : SQUAT_FLAG_NONFINITE;
-            }
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        unsigned char *to = codes + STEP * i * (D * BITS / 8);
-        if (BITS == 2) *reinterpret_cast<unsigned short *>(to) = (unsigned short)words[i];
-        else *reinterpret_cast<unsigned *>(to) = words[i];
-    }
-    if (flags) atomicOr(p.status, flags);
+    if (part == 0) write_keys<G, BITS, BF16, M16>(p, src, slots);
+    else write_values<G, BITS, BF16, M16>(p, src, slots);
 }
 
 // Keys that squat_quantize_keys has left in the workspace, [heads, tokens]: codes x[0], metadata x[1] (scales, then zero-points
 // y[0]); a group's codes are one span on either side.
 template <int G, int BITS, bool M16>
-__global__ void __launch_bounds__(128) pages_place_kernel(PagesParams p, int n_groups)
+__global__ void __launch_bounds__(128) pages_place_kernel(PagesParams p)
 {
     const int h = blockIdx.y, tid = threadIdx.x;
     const unsigned char *codes = static_cast<const unsigned char *>(p.x[0]);
     const void *scales = p.x[1], *zeros = p.y[0];
     const int *slots = p.slots;
     grid_wait(codes, scales, zeros, slots);
-    const long long tok = group_token<G>(p, slots, h);
+    const long long tok = group_token<G>(p, slots, blockIdx.x, h);
     if (tok < 0) return;
-    const long long from = (long long)h * n_groups + blockIdx.x;
+    const long long from = (long long)h * p.n_groups + blockIdx.x;
     constexpr int CODES16 = G * BITS, META16 = D * (M16 ? 2 : 4) / 16;       // 16-byte pieces
     const uint4 *src = reinterpret_cast<const uint4 *>(codes) + from * CODES16;
     uint4 *dst = reinterpret_cast<uint4 *>(p.pool.kc + tok * (D * BITS / 8));
@@ -251,44 +429,77 @@ __global__ void __launch_bounds__(128) pages_place_kernel(PagesParams p, int n_g
     }
 }
 
-// grid (groups, heads, keys / values); threads as for the write
-template <int G, int BITS, bool BF16, bool M16>
-__global__ void __launch_bounds__(4 * G) pages_read_kernel(PagesParams p)
+// Channels 2 I, 2 I + 1 of a thread's eight codes as two exact floats: a code, masked where it stands at bit s, under the exponent of
+// 2^(23 - s) makes 2^(23 - s) + code, and the subtraction of the bias leaves the code.  4-bit codes 4 .. 7 are taken from word >> 16.
+template <int BITS, int I>
+__device__ __forceinline__ u64 codes_as_floats(unsigned word)
 {
-    constexpr int STEP = G / ROWS;
-    const int part = p.first + blockIdx.z, h = blockIdx.y, tid = threadIdx.x, c8 = tid & 15, r0 = tid >> 4;
+    constexpr int S0 = (BITS * 2 * I) % 16, S1 = (BITS * (2 * I + 1)) % 16;
+    constexpr unsigned FIELD = (1u << BITS) - 1u, B0 = (unsigned)(150 - S0) << 23, B1 = (unsigned)(150 - S1) << 23;
+    const unsigned w = BITS == 4 && I >= 2 ? word >> 16 : word;
+    return fsub2(pack2(__uint_as_float((w & FIELD << S0) | B0), __uint_as_float((w & FIELD << S1) | B1)), pack2(__uint_as_float(B0), __uint_as_float(B1)));
+}
+
+// grid (runs of tokens, heads, keys / values): a thread takes eight channels of eight consecutive tokens, which lie in one
+// group, so the eight scales and zero-points of a key group are read once for all of them; a half-warp's stores are whole rows
+template <int G, int BITS, bool BF16, bool M16>
+__global__ void __launch_bounds__(READ_THREADS, 4) pages_read_kernel(PagesParams p)
+{
+    constexpr int TOK = 8;
+    const int part = p.first + blockIdx.z, h = blockIdx.y, c8 = threadIdx.x & 15;
+    const long long run = (long long)blockIdx.x * (READ_THREADS / 16) + (threadIdx.x >> 4);
+    const int group = (int)(run / (G / TOK)), in_group = (int)(run % (G / TOK)) * TOK;
     const unsigned char *codes = part == 0 ? p.pool.kc : p.pool.vc;
     const void *scales = part == 0 ? p.pool.ks : p.pool.vs, *zeros = part == 0 ? p.pool.kz : p.pool.vz;
     const int *slots = p.slots;
     grid_wait(codes, scales, zeros, slots);
-    const long long tok = group_token<G>(p, slots, h);
+    if (group >= p.n_groups) return;
+    long long tok = group_token<G>(p, slots, group, h);
     if (tok < 0) return;
-    unsigned words[ROWS];
+    tok += in_group;
+    unsigned words[TOK];
+    const unsigned char *from = codes + tok * (D * BITS / 8) + c8 * BITS;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const unsigned char *from = codes + (tok + r0 + STEP * i) * (D * BITS / 8) + c8 * BITS;
-        words[i] = BITS == 2 ? (unsigned)__ldg(reinterpret_cast<const unsigned short *>(from)) : __ldg(reinterpret_cast<const unsigned *>(from));
-    }
-    float s[8], z[8];
+    for (int i = 0; i < TOK; ++i)
+        words[i] = BITS == 2 ? (unsigned)__ldg(reinterpret_cast<const unsigned short *>(from + i * (D * BITS / 8))) : __ldg(reinterpret_cast<const unsigned *>(from + i * (D * BITS / 8)));
+    u64 s2[4], z2[4];                            // of the channels (keys)
+    float sv[TOK], zv[TOK];                      // of the tokens (values)
     if (part == 0) {
+        const long long at = tok / G * D + 8 * c8;
+        if (M16) {
+            const uint4 a = ldg128(static_cast<const __half *>(scales) + at), b = ldg128(static_cast<const __half *>(zeros) + at);
+            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            s[c] = load_meta<M16>(scales, tok / G * D + 8 * c8 + c);
-            z[c] = load_meta<M16>(zeros, tok / G * D + 8 * c8 + c);
+            for (int c = 0; c < 4; ++c) {
+                const float2 u = __half22float2(*reinterpret_cast<const __half2 *>(&aw[c])), v = __half22float2(*reinterpret_cast<const __half2 *>(&bw[c]));
+                s2[c] = pack2(u.x, u.y);
+                z2[c] = pack2(v.x, v.y);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float4 u = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(scales) + at) + c), v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(zeros) + at) + c);
+                s2[2 * c] = pack2(u.x, u.y); s2[2 * c + 1] = pack2(u.z, u.w);
+                z2[2 * c] = pack2(v.x, v.y); z2[2 * c + 1] = pack2(v.z, v.w);
+            }
+        }
+    } else {
+        const long long at = tok * (D / G) + c8 / (G / 8);
+#pragma unroll
+        for (int i = 0; i < TOK; ++i) {
+            sv[i] = load_meta<M16>(scales, at + i * (D / G));
+            zv[i] = load_meta<M16>(zeros, at + i * (D / G));
         }
     }
+    const long long at = ((long long)group * G + in_group) * p.xt[part] + (long long)h * p.xh[part] + 8 * c8;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        if (part == 1) {
-            const long long at = (tok + r0 + STEP * i) * (D / G) + c8 / (G / 8);
-            s[0] = load_meta<M16>(scales, at);
-            z[0] = load_meta<M16>(zeros, at);
-        }
+    for (int i = 0; i < TOK; ++i) {
+        const u64 code2[4] = {codes_as_floats<BITS, 0>(words[i]), codes_as_floats<BITS, 1>(words[i]), codes_as_floats<BITS, 2>(words[i]), codes_as_floats<BITS, 3>(words[i])};
         float y[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-            y[c] = __fmaf_rn((float)(words[i] >> (BITS * c) & ((1u << BITS) - 1u)), part == 0 ? s[c] : s[0], part == 0 ? z[c] : z[0]);
-        const long long at = ((long long)blockIdx.x * G + r0 + STEP * i) * p.xt[part] + (long long)h * p.xh[part] + 8 * c8;
+        for (int c = 0; c < 4; ++c)
+            unpack2(part == 0 ? ffma2(code2[c], s2[c], z2[c]) : ffma2(code2[c], pack2(sv[i], sv[i]), pack2(zv[i], zv[i])), y[2 * c], y[2 * c + 1]);
+        const long long to = at + i * p.xt[part];
         if (BF16) {
             uint32_t w[4];
 #pragma unroll
@@ -296,11 +507,11 @@ __global__ void __launch_bounds__(4 * G) pages_read_kernel(PagesParams p)
                 const __nv_bfloat162 v = __floats2bfloat162_rn(y[2 * k], y[2 * k + 1]);
                 w[k] = *reinterpret_cast<const uint32_t *>(&v);
             }
-            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y[part]) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y[part]) + to) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
-            float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(p.y[part]) + at);
-            to[0] = make_float4(y[0], y[1], y[2], y[3]);
-            to[1] = make_float4(y[4], y[5], y[6], y[7]);
+            float4 *f = reinterpret_cast<float4 *>(static_cast<float *>(p.y[part]) + to);
+            f[0] = make_float4(y[0], y[1], y[2], y[3]);
+            f[1] = make_float4(y[4], y[5], y[6], y[7]);
         }
     }
 }
@@ -308,14 +519,15 @@ __global__ void __launch_bounds__(4 * G) pages_read_kernel(PagesParams p)
 template <int G, int BITS>
 int launch_inst(const PagesParams &p, bool write, dim3 grid, int dtype, int meta16, cudaStream_t st)
 {
-#define SQ_P(K, BF, MM) return squat_launch(K<G, BITS, BF, MM>, grid, 4 * G, 0, st, p)
     const bool bf = dtype == SQUAT_BF16;
+    grid.x = write ? (unsigned)((p.n_groups + Cta<G>::GROUPS - 1) / Cta<G>::GROUPS) : (unsigned)(((long long)p.n_groups * (G / 8) + READ_THREADS / 16 - 1) / (READ_THREADS / 16));
+#define SQ_P(K, T, BF, MM) return squat_launch(K<G, BITS, BF, MM>, grid, T, 0, st, p)
     if (write) {
-        if (bf) { if (meta16) SQ_P(pages_write_kernel, true, true); else SQ_P(pages_write_kernel, true, false); }
-        else { if (meta16) SQ_P(pages_write_kernel, false, true); else SQ_P(pages_write_kernel, false, false); }
+        if (bf) { if (meta16) SQ_P(pages_write_kernel, Cta<G>::THREADS, true, true); else SQ_P(pages_write_kernel, Cta<G>::THREADS, true, false); }
+        else { if (meta16) SQ_P(pages_write_kernel, Cta<G>::THREADS, false, true); else SQ_P(pages_write_kernel, Cta<G>::THREADS, false, false); }
     } else {
-        if (bf) { if (meta16) SQ_P(pages_read_kernel, true, true); else SQ_P(pages_read_kernel, true, false); }
-        else { if (meta16) SQ_P(pages_read_kernel, false, true); else SQ_P(pages_read_kernel, false, false); }
+        if (bf) { if (meta16) SQ_P(pages_read_kernel, READ_THREADS, true, true); else SQ_P(pages_read_kernel, READ_THREADS, true, false); }
+        else { if (meta16) SQ_P(pages_read_kernel, READ_THREADS, false, true); else SQ_P(pages_read_kernel, READ_THREADS, false, false); }
     }
 #undef SQ_P
 }
@@ -338,6 +550,7 @@ int squat_launch_pages(bool write, const squat_page_pool *pool, const int *slots
     PagesParams p;
     p.pool = page_pool_of(pool);
     p.slots = slots;
+    p.n_groups = n_groups;
     p.status = status;
     int parts = 0;
     p.first = 1;
@@ -351,7 +564,7 @@ int squat_launch_pages(bool write, const squat_page_pool *pool, const int *slots
         if (i == 0) p.first = 0;
     }
     if (parts == 0) return SQUAT_OK;
-    return launch_sized(p, write, dim3((unsigned)n_groups, (unsigned)pool->n_kv_heads, (unsigned)parts), pool, dtype, st);
+    return launch_sized(p, write, dim3(1, (unsigned)pool->n_kv_heads, (unsigned)parts), pool, dtype, st);
 }
 
 int squat_launch_pages_place(const squat_page_pool *pool, const int *slots, int n_groups, const void *codes, const void *scales,
@@ -360,13 +573,14 @@ int squat_launch_pages_place(const squat_page_pool *pool, const int *slots, int 
     PagesParams p;
     p.pool = page_pool_of(pool);
     p.slots = slots;
+    p.n_groups = n_groups;
     p.status = status;
     p.first = 0;
     p.x[0] = codes;
     p.x[1] = scales;
     p.y[0] = const_cast<void *>(zeros);
     const dim3 grid((unsigned)n_groups, (unsigned)pool->n_kv_heads);
-#define SQ_P(GG, BB) return pool->meta16 ? squat_launch(pages_place_kernel<GG, BB, true>, grid, 128, 0, st, p, n_groups) : squat_launch(pages_place_kernel<GG, BB, false>, grid, 128, 0, st, p, n_groups)
+#define SQ_P(GG, BB) return pool->meta16 ? squat_launch(pages_place_kernel<GG, BB, true>, grid, 128, 0, st, p) : squat_launch(pages_place_kernel<GG, BB, false>, grid, 128, 0, st, p)
     if (pool->bits == 2) { if (pool->group_size == 32) SQ_P(32, 2); if (pool->group_size == 64) SQ_P(64, 2); SQ_P(128, 2); }
     if (pool->group_size == 32) SQ_P(32, 4);
     if (pool->group_size == 64) SQ_P(64, 4);
