@@ -55,41 +55,6 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uin
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-template <bool BF>
-__device__ __forceinline__ uint32_t pack16(float lo, float hi)
-{
-    if (BF) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t *>(&v);
-    }
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
-__device__ __forceinline__ uint32_t as_u32(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
-// elements i of a and b (two to a word), as a pair
-__device__ __forceinline__ uint32_t pair16(uint32_t a, uint32_t b, int i) { return prmt(a, b, i & 1 ? 0x7632 : 0x5410); }
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Code c of the low half of `word` and of the high half, as a pair of binary16 numbers.
-template <int BITS>
-__device__ __forceinline__ __half2 code_pair(uint32_t word, int c)
-{
-    constexpr int IN_PLACE = BITS == 2 ? 5 : 2;      // codes whose bits lie within a binary16's significand as they are
-    const int s = BITS * (c < IN_PLACE ? c : c - IN_PLACE);
-    const uint32_t src = c < IN_PLACE ? word : word >> (BITS * IN_PLACE);
-    const uint32_t bias = (uint32_t)(25 - s) << 10 | (uint32_t)(25 - s) << 26, mask = ((1u << BITS) - 1u) * 0x00010001u << s;
-    return __hsub2(as_half2((src & mask) | bias), as_half2(bias));
-}
-template <int BITS>
-__device__ __forceinline__ float code_float(uint32_t word, int pos) { return (float)(word >> (BITS * pos) & ((1u << BITS) - 1u)); }
-
 // what a warp has seen of the magnitudes
 struct Range {
     __half2 ks, kz, vs, vz;                          // quantized scales and zero-points
@@ -265,9 +230,6 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, const uint3
         }
     }
 }
-
-__device__ __forceinline__ uint32_t bf16_pair_to_f16(uint32_t x) { return pack16<false>(bf16lo_to_f32(x), bf16hi_to_f32(x)); }
-__device__ __forceinline__ bool bf16_pair_not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
 // A step of rows in full precision: rows u0 .. u0 + 31 of the sequence, of which row g of the item sees the first sees[0], row
 // g + 8 the first sees[1], and none more than `most`.
@@ -560,12 +522,12 @@ __global__ void __launch_bounds__(THREADS, 2) chunk_rows_kernel(const __grid_con
     }
 }
 
-// CTA c: the item that CTA c of the main kernel began and did not finish, if there is one.
+// CTA c: the item that CTA c of the main kernel began and did not finish, if there is one.  A warp takes a row, four channels a lane.
 template <int ROWS>
 __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant__ ChunkParams params)
 {
     __shared__ ChunkShared sh;
-    const int tid = threadIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     ChunkParams p = params;
     grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
     long long per, total;
@@ -579,37 +541,39 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
     const long long parts = (first + chunk_tiles<ROWS>(p, sq, pl.qt) - 1) / per - c + 1;
     const int row0 = pl.qt * ROWS, n_rows = min(ROWS, sq.nq * p.qpk - row0);
 #pragma unroll 1
-    for (int r = blockIdx.y; r < n_rows; r += gridDim.y) {
-        float m = -INFINITY, l = 0.0f, o = 0.0f;
+    for (int r = blockIdx.y * 4 + warp; r < n_rows; r += gridDim.y * 4) {
+        float m = -INFINITY, l = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         constexpr int AT_ONCE = 8;                   // parts whose loads are in flight together
 #pragma unroll 1
         for (long long i0 = 0; i0 < parts; i0 += AT_ONCE) {
             float2 v[AT_ONCE];
-            float x[AT_ONCE];
+            float4 x[AT_ONCE];
 #pragma unroll
             for (int i = 0; i < AT_ONCE; ++i) {
                 const bool in = i0 + i < parts;
                 const long long at = ((i0 + i == 0 ? 2 * c + 1 : 2 * (c + i0 + i)) * ROWS + r);
                 v[i] = in ? *reinterpret_cast<const float2 *>(p.ml + at * 2) : make_float2(-INFINITY, 0.0f);
-                x[i] = in ? p.part[at * D + tid] : 0.0f;
+                x[i] = in ? *reinterpret_cast<const float4 *>(p.part + at * D + 4 * lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
             float mn = m;
 #pragma unroll
             for (int i = 0; i < AT_ONCE; ++i) mn = max_nan(mn, v[i].x);
             const float use = mn == -INFINITY ? 0.0f : mn, f0 = exp2_fast(m - use);
             l *= f0;
-            o *= f0;
+            o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
 #pragma unroll
             for (int i = 0; i < AT_ONCE; ++i) {
                 const float f = exp2_fast(v[i].x - use);
                 l = fmaf(f, v[i].y, l);
-                o = fmaf(f, x[i], o);
+                o.x = fmaf(f, x[i].x, o.x); o.y = fmaf(f, x[i].y, o.y); o.z = fmaf(f, x[i].z, o.z); o.w = fmaf(f, x[i].w, o.w);
             }
             m = mn;
         }
         const int row = row0 + r, j = sq.q0 + row / p.qpk, hq = pl.h * p.qpk + row % p.qpk;
-        p.out[(long long)j * p.ot + (long long)hq * p.oh + tid] = __float2bfloat16_rn(l == 0.0f ? 0.0f : o / l);
-        if (p.lse && tid == 0) p.lse[(long long)j * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        *reinterpret_cast<uint2 *>(p.out + (long long)j * p.ot + (long long)hq * p.oh + 4 * lane) = make_uint2(pack16<true>(o.x * inv, o.y * inv), pack16<true>(o.z * inv, o.w * inv));
+        if (p.lse && lane == 0) p.lse[(long long)j * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
     }
 }
 
@@ -636,28 +600,69 @@ int squat_launch_chunk_rows(const ChunkParams &p, int bits, int meta16, cudaStre
 #undef SQ_C
 }
 
+namespace {
+
+// The kernels of a call: rows of the sequences with at most few_rows rows per KV head go to the kernel for few rows, those of the
+// others to the kernel for many, in tiles of 128 or 256.
+struct ChunkKernels {
+    bool rows;
+    int tiles;                                       // 0: no kernel for many rows
+};
+constexpr int FEW_ROWS = 16;
+
+ChunkKernels kernels_for(long long n_q, long long n_seqs, long long max_q, int qpk)
+{
+    ChunkKernels k;
+    const long long most = max_q * qpk;
+    k.tiles = most <= FEW_ROWS ? 0 : most <= 128 ? 1 : 2;
+    k.rows = k.tiles == 0 || n_q != n_seqs * max_q;  // sequences of one length, all of them in the other kernel
+    return k;
+}
+int matrix_ctas(int tiles) { return squat_sm_count() * (tiles == 2 ? 1 : 2); }
+size_t part_floats(int n_cta, int rows) { return 2 * (size_t)n_cta * rows * (D + 2); }
+void use_part(ChunkParams &p, float *at, int n_cta, int rows)
+{
+    p.n_cta = n_cta;
+    p.part = at;
+    p.ml = at + 2 * (size_t)n_cta * rows * D;
+}
+
+}  // namespace
+
 size_t squat_chunk_workspace_floats(int n_q, int n_q_heads, int n_kv_heads, int max_q)
 {
-    (void)n_q; (void)n_q_heads; (void)n_kv_heads; (void)max_q;
-    return 2 * (size_t)(2 * squat_sm_count()) * CHUNK_ROWS * (D + 2);
+    (void)n_q;
+    size_t n = part_floats(2 * squat_sm_count(), CHUNK_ROWS);
+    const int tiles = kernels_for(0, 0, max_q, n_q_heads / n_kv_heads).tiles;
+    if (tiles) n += part_floats(matrix_ctas(tiles), 128 * tiles);
+    return n;
 }
 
 int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, float *workspace, int max_q, cudaStream_t st)
 {
-    (void)max_q;
     p.pool = page_pool_of(pool);
     p.G = pool->group_size;
     p.H = pool->n_kv_heads;
     p.qpk = p.Hq / p.H;
     p.status = squat_status_word();
     if (!p.status) return SQUAT_ERR_CUDA;
-    p.min_rows = 1;
-    p.max_rows = 0x7fffffff;
-    p.n_cta = 2 * squat_sm_count();
-    p.min_tiles = 2;
-    p.part = workspace;
-    p.ml = workspace + 2 * (size_t)p.n_cta * CHUNK_ROWS * D;
-    const int rc = squat_launch_chunk_rows(p, pool->bits, pool->meta16, st);
-    if (rc != SQUAT_OK) return rc;
-    return squat_launch(chunk_combine_kernel<CHUNK_ROWS>, dim3((unsigned)p.n_cta, 4), D, 0, st, p);
+    const ChunkKernels k = kernels_for(p.n_q, p.n_seqs, max_q, p.qpk);
+    ChunkParams few = p, many = p;
+    few.min_rows = 1;
+    few.max_rows = k.tiles ? FEW_ROWS : 0x7fffffff;
+    few.min_tiles = 2;
+    use_part(few, workspace, 2 * squat_sm_count(), CHUNK_ROWS);
+    many.min_rows = k.rows ? FEW_ROWS + 1 : 1;
+    many.max_rows = 0x7fffffff;
+    many.min_tiles = 4;
+    int rc = SQUAT_OK;
+    if (k.tiles) {
+        use_part(many, workspace + part_floats(few.n_cta, CHUNK_ROWS), matrix_ctas(k.tiles), 128 * k.tiles);
+        rc = squat_launch_chunk_matrix(many, k.tiles, pool->bits, pool->meta16, st);
+    }
+    if (rc == SQUAT_OK && k.rows) rc = squat_launch_chunk_rows(few, pool->bits, pool->meta16, st);
+    if (rc == SQUAT_OK && k.tiles == 1) rc = squat_launch(chunk_combine_kernel<128>, dim3((unsigned)many.n_cta, 8), D, 0, st, many);
+    if (rc == SQUAT_OK && k.tiles == 2) rc = squat_launch(chunk_combine_kernel<256>, dim3((unsigned)many.n_cta, 16), D, 0, st, many);
+    if (rc == SQUAT_OK && k.rows) rc = squat_launch(chunk_combine_kernel<CHUNK_ROWS>, dim3((unsigned)few.n_cta, 1), D, 0, st, few);
+    return rc;
 }

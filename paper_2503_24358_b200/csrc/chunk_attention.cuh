@@ -150,5 +150,46 @@ __device__ __forceinline__ void chunk_next(const ChunkParams &p, ChunkPlace &w, 
     } while (s.nq == 0);
 }
 
+// ---- pairs of 16-bit numbers
+template <bool BF>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi)
+{
+    if (BF) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
+__device__ __forceinline__ uint32_t as_u32(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) { return __byte_perm(a, b, sel); }
+// elements i of a and b (two to a word), as a pair
+__device__ __forceinline__ uint32_t pair16(uint32_t a, uint32_t b, int i) { return prmt(a, b, i & 1 ? 0x7632 : 0x5410); }
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Code c of the low half of `word` and of the high half, as a pair of binary16 numbers.
+template <int BITS>
+__device__ __forceinline__ __half2 code_pair(uint32_t word, int c)
+{
+    constexpr int IN_PLACE = BITS == 2 ? 5 : 2;      // codes whose bits lie within a binary16's significand as they are
+    const int s = BITS * (c < IN_PLACE ? c : c - IN_PLACE);
+    const uint32_t src = c < IN_PLACE ? word : word >> (BITS * IN_PLACE);
+    const uint32_t bias = (uint32_t)(25 - s) << 10 | (uint32_t)(25 - s) << 26, mask = ((1u << BITS) - 1u) * 0x00010001u << s;
+    return __hsub2(as_half2((src & mask) | bias), as_half2(bias));
+}
+template <int BITS>
+__device__ __forceinline__ float code_float(uint32_t word, int pos) { return (float)(word >> (BITS * pos) & ((1u << BITS) - 1u)); }
+
+__device__ __forceinline__ uint32_t bf16_pair_to_f16(uint32_t x) { return pack16<false>(bf16lo_to_f32(x), bf16hi_to_f32(x)); }
+__device__ __forceinline__ bool bf16_pair_not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+
+
 constexpr int CHUNK_ROWS = 16;                       // rows of an item in the kernel for few rows
+int squat_launch_chunk_matrix(const ChunkParams &p, int tiles, int bits, int meta16, cudaStream_t st);
 int squat_launch_chunk_rows(const ChunkParams &p, int bits, int meta16, cudaStream_t st);

@@ -1,0 +1,619 @@
+// Attention of new tokens over a paged, quantized cache: the kernel for many rows per KV head (chunks of prompts, drafts under
+// grouped queries).  The formulas are those of chunk_attention.cu; here a row's work is enough for the tensor cores to bound it.
+//
+// An item is 128 or 256 rows (TILES tiles of 128) of one KV head.  Roles of a CTA's warps, handing tiles of 128 tokens on through
+// mbarriers:
+//   producers (4 warps)  dequantize keys and values into shared memory, binary16 in the 128-byte swizzle, once for all rows of the
+//                        item: a thread takes 16 channels of a token, eight tokens of one group of keys, whose scales it holds.
+//   products (1 thread)  S = Q K^T into tensor memory, then O += P V with P taken from tensor memory; per tile of rows in the order
+//                        PV(j), QK(j + 1), so that the scores of one tile are made while the other tile's warps work on theirs.
+//   softmax (4 warps a tile)  a thread owns a row: maximum, weights 2^(c s - m + 8), written over its scores as binary16, and the
+//                        denominator.  The sum in tensor memory is rescaled only when the maximum has grown by more than 2^6
+//                        (weights then reach 2^14, within binary16).
+// Channels stand in the order that the dequantization leaves them in (the two codes 16 bits apart in a word are neighbours); the
+// queries are stored the same way and the result is put in order when it is written.
+// Magnitudes beyond binary16 are noticed on the way, and the segment is done again with bf16 operands.
+#include "chunk_attention.cuh"
+
+namespace {
+
+constexpr int D = SQUAT_D, T = CHUNK_TILE;
+constexpr float P_SHIFT = 8.0f, GROW = 6.0f;
+constexpr int OPERAND = T * D * 2;                   // bytes of a tile of 128 rows in shared memory: two halves of 64 channels
+
+template <int TILES>
+struct Plan {
+    static constexpr int ROWS = 128 * TILES, STAGES = TILES, SOFT = 128 * TILES, THREADS = SOFT + 128 + 32;
+    static constexpr int CTAS = TILES == 2 ? 1 : 2;  // to an SM
+    static constexpr int TMEM = 256 * TILES;         // columns: scores (and weights) of each tile, then sums of each tile
+    static constexpr size_t SMEM = 1024 + (size_t)(TILES + 2 * STAGES) * OPERAND;
+};
+
+// 128 rows of 64 elements of 16 bits, 128-byte swizzle, groups of 8 rows 1024 bytes apart.  Contraction along the row (queries,
+// keys), or across rows (values: 64 channels per row, the next 64 OPERAND / 2 further on).
+__device__ __forceinline__ u64 rows_desc(unsigned addr) { return (u64)((addr & 0x3FFFF) >> 4) | ((u64)1 << 16) | ((u64)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61); }
+__device__ __forceinline__ u64 columns_desc(unsigned addr) { return (u64)((addr & 0x3FFFF) >> 4) | ((u64)((OPERAND / 2) >> 4) << 16) | ((u64)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61); }
+// float32 accumulator, both operands binary16 or both bf16, M = N = 128, B with the contraction along its rows or across them
+__device__ __forceinline__ unsigned idesc_16(bool bf, bool b_across)
+{
+    return (1u << 4) | (bf ? (1u << 7) | (1u << 10) : 0u) | (b_across ? 1u << 16 : 0u) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(unsigned d, u64 a, u64 b, unsigned idesc, unsigned accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(unsigned d, unsigned a, u64 b, unsigned idesc, unsigned accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(unsigned addr, float (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]),
+                   "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]),
+                   "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(unsigned addr, const float (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(addr), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]),
+                   "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]),
+                   "f"(r[30]), "f"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(unsigned addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+                   "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void mbar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void mbar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// What a CTA's roles share besides the operands
+template <int TILES>
+struct Shared {
+    u64 k_full[Plan<TILES>::STAGES], k_empty[Plan<TILES>::STAGES], v_full[Plan<TILES>::STAGES], v_empty[Plan<TILES>::STAGES];
+    u64 s_full[TILES], p_full[TILES], o_full[TILES];
+    unsigned tmem;
+    int failed;                                      // a bounded wait ran out: no more waits, the results are not valid
+    int wide;                                        // binary16 is too narrow for the segment
+    int odd_first, odd_last;                         // range of rows in full precision that hold infinities or NaN among their values
+    int v_top, k_top;                                // largest magnitudes, as float bits
+    ChunkShared place;
+};
+
+// Waits at most once the limit's time in all: after one wait that ran out, none is taken any more.
+__device__ __forceinline__ void wait_for(u64 &bar, unsigned parity, int &failed, unsigned *status)
+{
+    if (*(volatile int *)&failed) return;
+    if (mbar_wait(smem_u32(&bar), parity)) return;
+    failed = 1;
+    atomicOr(status, SQUAT_FLAG_DEVICE_TIMEOUT);
+}
+
+// 16 channels of a token in the operand: two 16-byte pieces.  Lanes of the upper half store the second one first, so that eight lanes
+// of a token fall on distinct banks.
+__device__ __forceinline__ void store_unit(unsigned char *operand, int row, int unit, const uint32_t (&r)[8])
+{
+    unsigned char *base = operand + unit / 4 * (OPERAND / 2) + row * 128;
+    const int c = unit % 4 * 2, first = unit / 4;
+    const uint4 a = make_uint4(r[0], r[1], r[2], r[3]), b = make_uint4(r[4], r[5], r[6], r[7]);
+    *reinterpret_cast<uint4 *>(base + (((c + first) ^ (row & 7)) << 4)) = first ? b : a;
+    *reinterpret_cast<uint4 *>(base + (((c + 1 - first) ^ (row & 7)) << 4)) = first ? a : b;
+}
+
+// 16 bf16 numbers, as loaded, in the operand's order
+template <int BITS>
+__device__ __forceinline__ void unit_of_bf16(const uint32_t (&x)[8], bool bf, uint32_t (&r)[8])
+{
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {
+        const uint32_t v = BITS == 2 ? pair16(x[m / 2], x[4 + m / 2], m) : pair16(x[m / 4 * 4 + m % 4 / 2], x[m / 4 * 4 + 2 + m % 4 / 2], m);
+        r[m] = bf ? v : bf16_pair_to_f16(v);
+    }
+}
+
+// Eight units of a thread (tokens 32 (thread / 32) + thread / 8 mod 4 + 4 i, unit thread mod 8): codes as loaded and what they need.
+template <int BITS>
+struct Units {
+    uint32_t code[8][BITS / 2];
+};
+
+template <int BITS, int G, bool M16, int TILES>
+struct Producer {
+    static constexpr int ROW = D * BITS / 8, NG = D / G;
+    const ChunkParams &p;
+    const ChunkSeq &sq;
+    int h, most, ct, group32, sub, unit;             // the thread's 32 tokens of a tile, its first of them, its channels
+
+    // first token of the thread's 32 in the pool for tile t; -1: past the cached tokens
+    __device__ __forceinline__ long long place(int seq, int t) const
+    {
+        const int at = t * T + 32 * group32;
+        if (t >= ct || at >= sq.cached) return -1;
+        const int pg = at / p.pool.page_tokens;
+        int page = __ldg(p.page_table + (long long)seq * p.table_stride + pg);
+        if ((unsigned)page >= (unsigned)p.pool.n_pages) {
+            atomicOr(p.status, SQUAT_FLAG_PAGES);
+            page = 0;
+        }
+        return (long long)page * p.pool.page_stride + (long long)h * p.pool.head_stride + (at - pg * p.pool.page_tokens);
+    }
+    __device__ __forceinline__ void load_codes(const unsigned char *codes, long long tok, Units<BITS> &u) const
+    {
+        const unsigned char *from = codes + (tok + sub) * ROW + unit * (2 * BITS);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (BITS == 2) u.code[i][0] = __ldg(reinterpret_cast<const uint32_t *>(from + 4 * i * ROW));
+            else {
+                const uint2 v = __ldg(reinterpret_cast<const uint2 *>(from + 4 * i * ROW));
+                u.code[i][0] = v.x; u.code[i][BITS / 2 - 1] = v.y;
+            }
+        }
+    }
+    // the pair of codes that becomes register m of a unit
+    __device__ __forceinline__ static __half2 pair(const Units<BITS> &u, int i, int m) { return BITS == 2 ? code_pair<BITS>(u.code[i][0], m) : code_pair<BITS>(u.code[i][m / 4 * (BITS / 2 - 1)], m % 4); }
+    // channels (within the unit) of register m
+    __device__ __forceinline__ static int lo_of_reg(int m) { return BITS == 2 ? m : m / 4 * 8 + m % 4; }
+    __device__ __forceinline__ static int hi_of_reg(int m) { return lo_of_reg(m) + (BITS == 2 ? 8 : 4); }
+    __device__ __forceinline__ static float code_at(const Units<BITS> &u, int i, int c)
+    {
+        return BITS == 2 ? code_float<BITS>(u.code[i][0], c) : code_float<BITS>(u.code[i][c / 8 * (BITS / 2 - 1)], c % 8);
+    }
+};
+
+template <int BITS, int G, bool M16, int TILES>
+__global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk_matrix_kernel(const __grid_constant__ ChunkParams params)
+{
+    using S = Plan<TILES>;
+    using Pr = Producer<BITS, G, M16, TILES>;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Shared<TILES> sh;
+    unsigned char *q_sm = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024, *k_sm = q_sm + TILES * OPERAND, *v_sm = k_sm + S::STAGES * OPERAND;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    constexpr int SOFT_WARPS = S::SOFT / 32, MMA_WARP = SOFT_WARPS + 4;
+    ChunkParams p = params;
+    grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
+    long long per, total;
+    chunk_share<S::ROWS>(p, sh.place, per, total);
+    long long at = per * blockIdx.x;
+    if (at >= total) return;
+    const long long end = min(at + per, total);
+    ChunkPlace pl = chunk_locate<S::ROWS>(p, sh.place, at);
+    ChunkSeq sq = chunk_seq(p, pl.seq);
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"((unsigned)S::TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (tid == 0) {
+        for (int i = 0; i < S::STAGES; ++i) {
+            mbar_init(smem_u32(&sh.k_full[i]), 128);
+            mbar_init(smem_u32(&sh.v_full[i]), 128);
+            mbar_init(smem_u32(&sh.k_empty[i]), 1);
+            mbar_init(smem_u32(&sh.v_empty[i]), 1);
+        }
+        for (int t = 0; t < TILES; ++t) {
+            mbar_init(smem_u32(&sh.s_full[t]), 1);
+            mbar_init(smem_u32(&sh.p_full[t]), 128);
+            mbar_init(smem_u32(&sh.o_full[t]), 1);
+        }
+        sh.failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const unsigned tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
+    unsigned kv = 0, turns = 0, segments = 0;        // tiles of tokens, scores of a row tile, and segments so far
+
+    while (at < end) {
+        const int tiles = chunk_tiles<S::ROWS>(p, sq, pl.qt), ta = pl.tile, tb = (int)min((long long)tiles, ta + (end - at)), n = tb - ta;
+        const int rows = sq.nq * p.qpk, row0 = pl.qt * S::ROWS, n_rows = min(S::ROWS, rows - row0), last = row0 + n_rows - 1;
+        const int ct = (sq.cached + T - 1) / T, most = chunk_sees(p, sq, last / p.qpk);
+        bool bf = false;
+        for (;;) {
+            if (tid == 0) {
+                sh.wide = 0;
+                sh.odd_first = 0x7fffffff;
+                sh.odd_last = -1;
+                sh.v_top = sh.k_top = 0;
+            }
+            __syncthreads();
+            // ---------------------------------------------------------------- queries, a thread a row
+            if (tid < S::SOFT) {
+                const int r = tid;
+                float top = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8];
+                    if (r < n_rows) {
+                        const __nv_bfloat16 *from = p.q + (long long)(sq.q0 + (row0 + r) / p.qpk) * p.qt + (long long)(pl.h * p.qpk + (row0 + r) % p.qpk) * p.qh + 16 * u;
+                        const uint4 a = ldg128(from), b = ldg128(from + 8);
+                        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(bf16lo_to_f32(x[i])), fabsf(bf16hi_to_f32(x[i]))));
+                    unit_of_bf16<BITS>(x, bf, y);
+                    unsigned char *base = q_sm + r / 128 * OPERAND + u / 4 * (OPERAND / 2) + r % 128 * 128;
+                    *reinterpret_cast<uint4 *>(base + ((u % 4 * 2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<uint4 *>(base + (((u % 4 * 2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+                }
+                if (!(top < 4096.0f)) sh.wide = 1;
+                fence_async_smem();
+            }
+            __syncthreads();
+
+            if (warp < SOFT_WARPS) {
+                // ------------------------------------------------------------ softmax
+                const int t = warp / 4, r = tid;
+                const unsigned s_addr = tmem + 128 * t + ((unsigned)(warp % 4 * 32) << 16), o_addr = tmem + 128 * (TILES + t) + ((unsigned)(warp % 4 * 32) << 16);
+                const int sees = chunk_sees(p, sq, min(row0 + r, last) / p.qpk);
+                float m = -INFINITY, l = 0.0f;
+                const float c = p.scale_log2;
+#pragma unroll 1
+                for (int j = 0; j < n; ++j) {
+                    const int tile = ta + j, lim = tile < ct ? sq.cached - tile * T : sees - (tile - ct) * T;
+                    const bool masked = __any_sync(0xffffffffu, lim < T);
+                    wait_for(sh.s_full[t], (turns + j) & 1, sh.failed, p.status);
+                    tc_fence_after();
+                    float x[32], mx = -INFINITY;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        tmem_ld32(s_addr + 32 * b, x);
+                        tmem_ld_wait();
+                        if (masked)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = 32 * b + i < lim ? x[i] : -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, x[i]);
+                    }
+                    mx *= c;
+                    if (j == 0) m = mx;
+                    else if (__any_sync(0xffffffffu, mx > m + GROW)) {
+                        const float top = mx > m + GROW ? mx : m, use = top == -INFINITY ? 0.0f : top, f = exp2_fast(m - use);
+                        m = top;
+                        l *= f;
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            tmem_ld32(o_addr + 32 * b, x);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] *= f;
+                            tmem_st32(o_addr + 32 * b, x);
+                        }
+                    }
+                    const float base = P_SHIFT - (m == -INFINITY ? 0.0f : m);
+                    const u64 c2 = pack2(c, c), base2 = pack2(base, base);
+                    u64 sum2 = 0;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        tmem_ld32(s_addr + 32 * b, x);
+                        tmem_ld_wait();
+                        if (masked)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = 32 * b + i < lim ? x[i] : -INFINITY;
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float y0, y1;
+                            unpack2(ffma2(pack2(x[2 * i], x[2 * i + 1]), c2, base2), y0, y1);
+                            y0 = exp2_fast(y0);
+                            y1 = exp2_fast(y1);
+                            sum2 = fadd2(sum2, pack2(y0, y1));
+                            w[i] = bf ? pack16<true>(y0, y1) : pack16<false>(y0, y1);
+                        }
+                        tmem_st16(s_addr + 16 * b, w);
+                    }
+                    l += lo_of(sum2) + hi_of(sum2);
+                    tmem_st_wait();
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&sh.p_full[t]));
+                }
+                wait_for(sh.o_full[t], segments & 1, sh.failed, p.status);
+                tc_fence_after();
+                // ------------------------------------------------------------ result: of the segment (`wide` and the values' range are known)
+                const float v_top = __int_as_float(*(volatile int *)&sh.v_top);
+                const bool again = !bf && (*(volatile int *)&sh.wide || !(__int_as_float(*(volatile int *)&sh.k_top) < 4096.0f) || !(v_top < 65000.0f) || (v_top < 0x1p-8f && v_top > 0.0f));
+                if (!again) {
+                    const bool whole = ta == 0 && tb == tiles;
+                    const long long slot = 2LL * blockIdx.x + (ta == 0 ? 1 : 0);
+                    const int row = row0 + r, q_row = sq.q0 + row / p.qpk, hq = pl.h * p.qpk + row % p.qpk;
+                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                    const int odd_first = max(sh.odd_first, (max(ta, ct) - ct) * T), odd_last = min(sh.odd_last, sees - 1);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        float x[32];
+                        __syncwarp();
+                        tmem_ld32(o_addr + 32 * b, x);
+                        tmem_ld_wait();
+                        if (r >= n_rows) continue;
+                        float y[32];                 // in the order of the channels
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const int e = i % 16, at_reg = BITS == 2 ? 2 * (e % 8) + e / 8 : e / 8 * 8 + 2 * (e % 4) + e % 8 / 4;
+                            y[i] = l == 0.0f ? 0.0f : x[i / 16 * 16 + at_reg];
+                        }
+                        for (int u = odd_first; u <= odd_last; ++u) {       // rare: infinities and NaN that the row sees
+                            const __nv_bfloat16 *v = p.v_new + (long long)(sq.k0 + u) * p.vnt + (long long)pl.h * p.vnh + 32 * b;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const float o = __bfloat162float(v[i]);
+                                if (!(fabsf(o) < INFINITY)) y[i] += o;
+                            }
+                        }
+                        if (whole) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = pack16<true>(y[2 * i] * inv, y[2 * i + 1] * inv);
+                            uint4 *to = reinterpret_cast<uint4 *>(p.out + (long long)q_row * p.ot + (long long)hq * p.oh + 32 * b);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) to[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                        } else {
+                            float4 *to = reinterpret_cast<float4 *>(p.part + (slot * S::ROWS + r) * D + 32 * b);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                        }
+                    }
+                    if (r < n_rows) {
+                        if (!whole) *reinterpret_cast<float2 *>(p.ml + (slot * S::ROWS + r) * 2) = make_float2(m, l);
+                        else if (p.lse) p.lse[(long long)q_row * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
+                    }
+                }
+                tc_fence_before();
+            } else if (warp < MMA_WARP) {
+                // ------------------------------------------------------------ producers
+                const int pt = tid - S::SOFT;
+                const Pr pr{p, sq, pl.h, most, ct, pt / 32, pt / 8 % 4, pt % 8};
+                const int row0_sm = 32 * pr.group32 + pr.sub;
+                __half2 ks_top = __float2half2_rn(0.0f), kz_top = ks_top, vs_top = ks_top, vz_top = ks_top;
+                float k_top = 0.0f, v_top = 0.0f;
+                // what the segment's magnitudes were: before the last tile is handed on, so that who waits for its sums knows them
+                auto publish = [&]() {
+                    if (bf) return;
+                    constexpr float L = float((1 << BITS) - 1);
+                    auto top = [](__half2 x) { const float2 f = __half22float2(x); return fmaxf(f.x, f.y); };
+                    atomicMax(&sh.k_top, __float_as_int(fmaxf(fmaf(L, top(ks_top), top(kz_top)), k_top)));
+                    atomicMax(&sh.v_top, __float_as_int(fmaxf(fmaf(L, top(vs_top), top(vz_top)), v_top)));
+                };
+                long long next = pr.place(pl.seq, ta);
+#pragma unroll 1
+                for (int j = 0; j < n; ++j) {
+                    const int tile = ta + j, stage = (kv + j) % S::STAGES;
+                    const unsigned parity = (((kv + j) / S::STAGES) & 1) ^ 1;
+                    unsigned char *k_to = k_sm + stage * OPERAND, *v_to = v_sm + stage * OPERAND;
+                    const long long tok = next;
+                    if (j + 1 < n) next = pr.place(pl.seq, tile + 1);
+                    if (tile < ct) {
+                        Units<BITS> ku, vu;
+                        float sc[16], zr[16], vsc[8], vzr[8];
+                        if (tok >= 0) {
+                            pr.load_codes(p.pool.kc, tok, ku);
+                            const long long mk = tok / G * D + 16 * pr.unit;
+                            if (M16) {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const uint4 a = ldg128(static_cast<const __half *>(p.pool.ks) + mk + 8 * i), b = ldg128(static_cast<const __half *>(p.pool.kz) + mk + 8 * i);
+                                    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const float2 u = __half22float2(as_half2(aw[e])), v = __half22float2(as_half2(bw[e]));
+                                        sc[8 * i + 2 * e] = u.x; sc[8 * i + 2 * e + 1] = u.y;
+                                        zr[8 * i + 2 * e] = v.x; zr[8 * i + 2 * e + 1] = v.y;
+                                    }
+                                }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    *reinterpret_cast<float4 *>(sc + 4 * i) = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(p.pool.ks) + mk) + i);
+                                    *reinterpret_cast<float4 *>(zr + 4 * i) = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(p.pool.kz) + mk) + i);
+                                }
+                            }
+                            pr.load_codes(p.pool.vc, tok, vu);
+                            const long long mv = (tok + pr.sub) * Pr::NG + 16 * pr.unit / G;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                vsc[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(p.pool.vs) + mv + 4 * i * Pr::NG)) : __ldg(static_cast<const float *>(p.pool.vs) + mv + 4 * i * Pr::NG);
+                                vzr[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(p.pool.vz) + mv + 4 * i * Pr::NG)) : __ldg(static_cast<const float *>(p.pool.vz) + mv + 4 * i * Pr::NG);
+                            }
+                        }
+                        wait_for(sh.k_empty[stage], parity, sh.failed, p.status);
+                        if (tok < 0) {               // behind the last cached token: zeros
+                            const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) store_unit(k_to, row0_sm + 4 * i, pr.unit, zero);
+                        } else if (!bf) {
+                            __half2 s2[8], z2[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                s2[e] = __floats2half2_rn(sc[Pr::lo_of_reg(e)], sc[Pr::hi_of_reg(e)]);
+                                z2[e] = __floats2half2_rn(zr[Pr::lo_of_reg(e)], zr[Pr::hi_of_reg(e)]);
+                                ks_top = __hmax2(ks_top, __habs2(s2[e]));
+                                kz_top = __hmax2(kz_top, __habs2(z2[e]));
+                            }
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                uint32_t y[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(Pr::pair(ku, i, e), s2[e], z2[e]));
+                                store_unit(k_to, row0_sm + 4 * i, pr.unit, y);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                uint32_t y[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const int a = Pr::lo_of_reg(e), b = Pr::hi_of_reg(e);
+                                    y[e] = pack16<true>(fmaf(Pr::code_at(ku, i, a), sc[a], zr[a]), fmaf(Pr::code_at(ku, i, b), sc[b], zr[b]));
+                                }
+                                store_unit(k_to, row0_sm + 4 * i, pr.unit, y);
+                            }
+                        }
+                        fence_async_smem();
+                        mbar_arrive(smem_u32(&sh.k_full[stage]));
+                        wait_for(sh.v_empty[stage], parity, sh.failed, p.status);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                            if (tok >= 0) {
+                                const __half2 s2 = __float2half2_rn(vsc[i]), z2 = __float2half2_rn(vzr[i]);
+                                if (!bf) {
+                                    vs_top = __hmax2(vs_top, __habs2(s2));
+                                    vz_top = __hmax2(vz_top, __habs2(z2));
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(Pr::pair(vu, i, e), s2, z2));
+                                } else {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e)
+                                        y[e] = pack16<true>(fmaf(Pr::code_at(vu, i, Pr::lo_of_reg(e)), vsc[i], vzr[i]), fmaf(Pr::code_at(vu, i, Pr::hi_of_reg(e)), vsc[i], vzr[i]));
+                                }
+                            }
+                            store_unit(v_to, row0_sm + 4 * i, pr.unit, y);
+                        }
+                        if (j == n - 1) publish();
+                        fence_async_smem();
+                        mbar_arrive(smem_u32(&sh.v_full[stage]));
+                    } else {
+                        // rows in full precision
+                        const int u0 = (tile - ct) * T + row0_sm;
+#pragma unroll
+                        for (int side = 0; side < 2; ++side) {
+                            const __nv_bfloat16 *src = side == 0 ? p.k_new : p.v_new;
+                            const long long st = side == 0 ? p.knt : p.vnt, shd = side == 0 ? p.knh : p.vnh;
+                            if (side == 0) wait_for(sh.k_empty[stage], parity, sh.failed, p.status);
+                            else wait_for(sh.v_empty[stage], parity, sh.failed, p.status);
+#pragma unroll 2
+                            for (int i = 0; i < 8; ++i) {
+                                const int u = u0 + 4 * i;
+                                uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8];
+                                if (u < most) {
+                                    const __nv_bfloat16 *from = src + (long long)(sq.k0 + u) * st + (long long)pl.h * shd + 16 * pr.unit;
+                                    const uint4 a = ldg128(from), b = ldg128(from + 8);
+                                    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+                                }
+                                bool odd = false;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    if (side == 1 && bf16_pair_not_finite(x[e])) {     // a row that does not see it must not meet it
+                                        odd = true;
+                                        if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+                                        if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0x0000ffffu;
+                                    }
+                                    const float lo = fabsf(bf16lo_to_f32(x[e])), hi = fabsf(bf16hi_to_f32(x[e]));
+                                    if (side == 0) k_top = fmaxf(k_top, fmaxf(lo < INFINITY ? lo : 0.0f, hi < INFINITY ? hi : 0.0f));
+                                    else v_top = fmaxf(v_top, fmaxf(lo, hi));
+                                }
+                                if (odd) {
+                                    atomicMin(&sh.odd_first, u);
+                                    atomicMax(&sh.odd_last, u);
+                                }
+                                unit_of_bf16<BITS>(x, bf, y);
+                                store_unit(side == 0 ? k_to : v_to, row0_sm + 4 * i, pr.unit, y);
+                            }
+                            if (side == 1 && j == n - 1) publish();
+                            fence_async_smem();
+                            mbar_arrive(smem_u32(side == 0 ? &sh.k_full[stage] : &sh.v_full[stage]));
+                        }
+                    }
+                }
+            } else {
+                // ------------------------------------------------------------ products
+                const unsigned id_s = idesc_16(bf, false), id_o = idesc_16(bf, true);
+                auto scores = [&](int t, int stage) {
+                    const u64 a = rows_desc(smem_u32(q_sm + t * OPERAND)), b = rows_desc(smem_u32(k_sm + stage * OPERAND));
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const int off = (s / 4 * (OPERAND / 2) + s % 4 * 32) >> 4;
+                        mma_ss(tmem + 128 * t, a + off, b + off, id_s, s > 0);
+                    }
+                };
+                wait_for(sh.k_full[kv % S::STAGES], (kv / S::STAGES) & 1, sh.failed, p.status);
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        scores(t, kv % S::STAGES);
+                        tc_commit(smem_u32(&sh.s_full[t]));
+                    }
+                    tc_commit(smem_u32(&sh.k_empty[kv % S::STAGES]));
+                }
+                __syncwarp();
+#pragma unroll 1
+                for (int j = 0; j < n; ++j) {
+                    const int stage = (kv + j) % S::STAGES, next = (kv + j + 1) % S::STAGES;
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        if (t == 0) wait_for(sh.v_full[stage], ((kv + j) / S::STAGES) & 1, sh.failed, p.status);
+                        wait_for(sh.p_full[t], (turns + j) & 1, sh.failed, p.status);
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const u64 b = columns_desc(smem_u32(v_sm + stage * OPERAND));
+#pragma unroll
+                            for (int s = 0; s < 8; ++s) mma_ts(tmem + 128 * (TILES + t), tmem + 128 * t + 8 * s, b + (s * 2048 >> 4), id_o, j > 0 || s > 0);
+                            if (t == TILES - 1) tc_commit(smem_u32(&sh.v_empty[stage]));
+                            if (j + 1 == n) tc_commit(smem_u32(&sh.o_full[t]));
+                        }
+                        __syncwarp();
+                        if (j + 1 == n) continue;
+                        if (t == 0) {
+                            wait_for(sh.k_full[next], ((kv + j + 1) / S::STAGES) & 1, sh.failed, p.status);
+                            tc_fence_after();
+                        }
+                        if (elect_one()) {
+                            scores(t, next);
+                            tc_commit(smem_u32(&sh.s_full[t]));
+                            if (t == TILES - 1) tc_commit(smem_u32(&sh.k_empty[next]));
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+            kv += n;
+            turns += n;
+            ++segments;
+            __syncthreads();                         // (and the sums have been read)
+            tc_fence_after();
+            const float v_top = __int_as_float(sh.v_top);
+            const bool again = !bf && (sh.wide || !(__int_as_float(sh.k_top) < 4096.0f) || !(v_top < 65000.0f) || (v_top < 0x1p-8f && v_top > 0.0f));
+            __syncthreads();
+            if (!again) break;
+            bf = true;
+        }
+        at += n;
+        if (at < end) chunk_next<S::ROWS>(p, pl, sq);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((unsigned)S::TMEM) : "memory");
+}
+
+template <int BITS, int G, bool M16, int TILES>
+int launch_matrix(const ChunkParams &p, cudaStream_t st)
+{
+    using S = Plan<TILES>;
+    static std::atomic<unsigned long long> allowed{0};
+    const int rc = squat_allow_smem(reinterpret_cast<const void *>(chunk_matrix_kernel<BITS, G, M16, TILES>), S::SMEM, allowed);
+    if (rc != SQUAT_OK) return rc;
+    return squat_launch(chunk_matrix_kernel<BITS, G, M16, TILES>, p.n_cta, S::THREADS, S::SMEM, st, p);
+}
+template <int TILES>
+int launch_matrix_tiles(const ChunkParams &p, int bits, int meta16, cudaStream_t st)
+{
+#define SQ_C(BB, GG) return meta16 ? launch_matrix<BB, GG, true, TILES>(p, st) : launch_matrix<BB, GG, false, TILES>(p, st)
+    if (bits == 2) { if (p.G == 32) SQ_C(2, 32); if (p.G == 64) SQ_C(2, 64); SQ_C(2, 128); }
+    if (p.G == 32) SQ_C(4, 32);
+    if (p.G == 64) SQ_C(4, 64);
+    SQ_C(4, 128);
+#undef SQ_C
+}
+
+}  // namespace
+
+int squat_launch_chunk_matrix(const ChunkParams &p, int tiles, int bits, int meta16, cudaStream_t st)
+{
+    return tiles == 2 ? launch_matrix_tiles<2>(p, bits, meta16, st) : launch_matrix_tiles<1>(p, bits, meta16, st);
+}
