@@ -467,6 +467,8 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
  *   lse          NULL, or float32 [n_q, n_q_heads]: natural logarithm of the softmax's denominator.
  *   workspace    device, 256-byte aligned, at least squat_chunk_attention_workspace_bytes(...); nothing is kept in it between
  *                calls.  Calls that may run at the same time need workspaces of their own.
+ * Sums are cut into parts where all sequences' lengths put the borders between SMs: the same call gives the same bits, a sequence
+ * in other company may differ in the last bit.
  * Everything that changes from step to step is read on the device, so a captured call can be replayed with other lengths,
  * pages and row ranges (n_q, n_seqs and max_q as captured).  A length or row range outside its limits sets SQUAT_FLAG_PAGES and is
  * cut to them; for a page number outside the pool (the flag too) the result of that sequence is not defined.

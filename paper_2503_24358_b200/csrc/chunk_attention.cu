@@ -3,17 +3,20 @@
 //
 //   out_r = sum_t p_rt v_t / sum_t p_rt,   p_rt = 2^(c <q_r, k_t> - m_r),   c = softmax scale / ln 2,   m_r the running maximum
 //
-// The cache's bytes bound it, if the two to four instructions that a code costs can be issued meanwhile.  So nothing is
-// staged for the tensor core: the operands of mma.sync m16n8k16 are made in the registers where it wants them.
-//   - The 16 rows of an item are the M side.  A warp takes 32 tokens at a time (they lie in one page and one group of keys) and
-//     keeps its own maximum, denominator and sum; a CTA's warps are joined at the end.
-//   - Scores: lane (g, q) holds token 8 n + g, channels 32 q .. 32 q + 31: a contiguous quarter of its codes.  Which of them
-//     stand at which of the 16 steps of the contraction is free, as long as the queries agree: the two codes 16 bits apart in a
-//     word become a pair of binary16 numbers by one logic instruction (their bits under the exponent of 2^(10 - s) make 2^(10 - s) + code),
-//     one subtraction, and one multiply-add with the channel pair's scale and zero-point.
-//   - Values: the same lane holds tokens 16 k + 2 q, + 1, + 8, + 9, channels 16 g .. 16 g + 15.  The halves of two tokens' words
-//     are joined first, so a pair is one channel of two tokens, which is the order of this operand.
-//   - A step's codes and metadata come through shared memory by cp.async, a few steps ahead.
+// The cache's bytes bound it, if the two instructions that a code costs can be issued meanwhile.  So nothing is staged for
+// the tensor core: the operands of mma.sync m16n8k16 are made in the registers where it wants them, the dequantized ones once for
+// up to 32 rows, 8 rows a product (the tcgen05 form wants them in shared or tensor memory, and 128 rows to fill it).
+//   - A warp takes 32 tokens at a time (they lie in one page and one group of keys) and keeps its own maximum, denominator and
+//     sum; a CTA's warps are joined at the end.
+//   - Scores, transposed: tokens are the 16 side.  Lane (g, q) holds tokens g and g + 8, channels 32 q .. 32 q + 31: a contiguous
+//     quarter of their codes.  Which of them stand at which of the steps of the contraction is free, as long as the queries agree: the two
+//     codes 16 bits apart in a word become a pair of binary16 numbers by one logic instruction (their bits under the exponent of 2^(10 - s)
+//     make 2^(10 - s) + code), one subtraction, and one multiply-add with the channel pair's scale and zero-point.
+//   - The weights' 8 x 8 blocks are transposed by movmatrix into the other operand of the second product.
+//   - Values, transposed: channels are the 16 side.  Lane (g, q) holds tokens 16 k + 2 q, + 1, + 8, + 9, channels 16 g .. 16 g + 15.
+//     The halves of two tokens' words are joined first, so a pair is one channel of two tokens, which is the order of this operand.
+//     Its sums stand at the lane that holds the rows' maxima.
+//   - A step's codes and metadata come through shared memory by cp.async, two steps ahead.
 // Binary16 keeps 11 significant bits, three more than bf16: the result's own rounding to bf16 is what is left.  Magnitudes
 // beyond its range (or values that all lie below 2^-8, where it would lose them) are noticed on the way, and the
 // segment is done again with bf16 operands.  Weights carry a factor of 2^8, so that those down to 2^-32 of the largest are not lost.
@@ -22,20 +25,21 @@
 namespace {
 
 constexpr int D = SQUAT_D;
-constexpr int THREADS = 128, WARPS = 4, STEP = 32;   // tokens per warp and step
-constexpr int R = CHUNK_ROWS;
+constexpr int THREADS = 128, WARPS = 4, STEP = 32, STAGES = 3;     // tokens per warp and step, steps in shared memory
 constexpr float P_SHIFT = 8.0f;
 
-template <int BITS, int G, bool M16>
+template <int BITS, bool M16>
 struct Stage {                                       // one step's part of the cache, in shared memory
-    static constexpr int MS = M16 ? 2 : 4, ROW = D * BITS / 8, NG = D / G;
+    static constexpr int MS = M16 ? 2 : 4, ROW = D * BITS / 8;
     static constexpr int QUARTER = 32 * MS + 16;     // key metadata: padded, so that the four quarters fall on distinct banks
-    static constexpr int KC = 0, VC = STEP * ROW, KS = 2 * STEP * ROW, KZ = KS + 4 * QUARTER, VS = KZ + 4 * QUARTER, VZ = VS + STEP * NG * MS;
-    static constexpr int BYTES = VZ + STEP * NG * MS;
-    static constexpr int STAGES = 3;
+    static constexpr int KC = 0, VC = STEP * ROW, KS = 2 * STEP * ROW, KZ = KS + 4 * QUARTER, VS = KZ + 4 * QUARTER, VZ = VS + STEP * 4 * MS;
+    static constexpr int BYTES = VZ + STEP * 4 * MS;
 };
 constexpr int MERGE_ROW = D + 4;
-constexpr int MERGE_BYTES = WARPS * R * (MERGE_ROW + 2) * 4;
+template <int NT>
+constexpr int MERGE_BYTES = WARPS * 8 * NT * (MERGE_ROW + 2) * 4;
+template <int NT>
+constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;  // to an SM
 
 __device__ __forceinline__ void cp16(unsigned dst, const void *src)
 {
@@ -55,151 +59,198 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uin
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 8 x 8 block of 16-bit numbers, lane (g, q) holding columns 2 q, 2 q + 1 of row g: transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // what a warp has seen of the magnitudes
 struct Range {
     __half2 ks, kz, vs, vz;                          // quantized scales and zero-points
     float k, v;                                      // rows in full precision
 };
 
-struct Acc {
-    float m[2], l[2], o[16][4];
+// The other operand of the scores: rows 8 t + g, pairs 2 kk and 2 kk + 1 of the lane's channels.  In registers; with four times eight rows,
+// whose sums take half of them, in the warp's own shared memory.
+template <int NT>
+struct Queries {
+    static constexpr bool IN_SMEM = NT == 4;
+    static constexpr int BYTES = IN_SMEM ? NT * 16 * 32 * 4 : 0;
+    uint32_t reg[IN_SMEM ? 1 : NT * 16];
+    uint32_t *smem;                                  // the lane's place: [t][kk / 2][lane][4]
+    __device__ __forceinline__ void put(int t, const uint32_t (&x)[16])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (IN_SMEM) *reinterpret_cast<uint4 *>(smem + (t * 4 + i) * 128) = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) reg[IN_SMEM ? 0 : t * 16 + 4 * i + e] = x[4 * i + e];
+        }
+    }
+    __device__ __forceinline__ void get(int t, int kk, uint32_t (&b)[2]) const
+    {
+        if (IN_SMEM) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(smem + (t * 4 + kk / 2) * 128 + kk % 2 * 2);
+            b[0] = v.x; b[1] = v.y;
+        } else {
+            b[0] = reg[IN_SMEM ? 0 : t * 16 + 2 * kk];
+            b[1] = reg[IN_SMEM ? 0 : t * 16 + 2 * kk + 1];
+        }
+    }
 };
 
-// One 32-token step's softmax: scores s[n][.] (columns 8 n + 2 q, + 1 of rows g and g + 8) become weights, packed as the A operand.
-template <bool BF>
-__device__ __forceinline__ void softmax_step(Acc &acc, float (&s)[4][4], float scale_log2, uint32_t (&pa)[2][4])
+// Rows 8 t + 2 q and 8 t + 2 q + 1: maximum, denominator, and sums of channels 16 g + i and 16 g + i + 8 (o[t][i]: row, row + 1, each)
+template <int NT>
+struct Acc {
+    float m[NT][2], l[NT][2], o[NT][8][4];
+};
+
+// One 32-token step's softmax: scores s[t][k] (tokens 16 k + g, + 8 of the lane's two rows) become weights, packed as the operand of the
+// second product.
+template <int NT, bool BF>
+__device__ __forceinline__ void softmax_step(Acc<NT> &acc, float (&s)[NT][2][4], float scale_log2, uint32_t (&pb)[NT][2][2])
 {
-    float corr[2], base[2];
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        float mx = -INFINITY;
+    for (int t = 0; t < NT; ++t) {
+        float base[2], corr[2];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) mx = max_nan(mx, max_nan(s[n][2 * r], s[n][2 * r + 1]));
-        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        const float m = max_nan(acc.m[r], mx * scale_log2), use = m == -INFINITY ? 0.0f : m;
-        corr[r] = exp2_fast(acc.m[r] - use);
-        acc.m[r] = m;
-        base[r] = P_SHIFT - use;
-        acc.l[r] *= corr[r];
-    }
+        for (int r = 0; r < 2; ++r) {
+            float mx = max_nan(max_nan(s[t][0][r], s[t][0][2 + r]), max_nan(s[t][1][r], s[t][1][2 + r]));
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        acc.o[i][0] *= corr[0]; acc.o[i][1] *= corr[0];
-        acc.o[i][2] *= corr[1]; acc.o[i][3] *= corr[1];
-    }
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            s[n][e] = exp2_fast(fmaf(s[n][e], scale_log2, base[e >> 1]));
-            acc.l[e >> 1] += s[n][e];
+            for (int o = 4; o < 32; o <<= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const float m = max_nan(acc.m[t][r], mx * scale_log2), use = m == -INFINITY ? 0.0f : m;
+            corr[r] = exp2_fast(acc.m[t][r] - use);
+            acc.m[t][r] = m;
+            base[r] = P_SHIFT - use;
+            acc.l[t][r] *= corr[r];
         }
-        pa[n >> 1][(n & 1) * 2] = pack16<BF>(s[n][0], s[n][1]);
-        pa[n >> 1][(n & 1) * 2 + 1] = pack16<BF>(s[n][2], s[n][3]);
+        if (__any_sync(0xffffffffu, corr[0] != 1.0f || corr[1] != 1.0f)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                acc.o[t][i][0] *= corr[0]; acc.o[t][i][2] *= corr[0];
+                acc.o[t][i][1] *= corr[1]; acc.o[t][i][3] *= corr[1];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[t][k][e] = exp2_fast(fmaf(s[t][k][e], scale_log2, base[e & 1]));
+                acc.l[t][e & 1] += s[t][k][e];
+            }
+            pb[t][k][0] = transposed(pack16<BF>(s[t][k][0], s[t][k][1]));
+            pb[t][k][1] = transposed(pack16<BF>(s[t][k][2], s[t][k][3]));
+        }
     }
 }
 
-// A step of cached tokens, staged at `st`.
-template <int BITS, int G, bool M16, bool BF>
-__device__ __forceinline__ void cached_step(const unsigned char *st, const uint32_t (&qf)[8][4], float scale_log2, Acc &acc, Range &range)
+// Scales or zero-points of pairs 2 kk and 2 kk + 1 of the lane's 32 channels: channels (lo, lo + HALF) and (lo + 1, lo + 1 + HALF).
+template <int BITS, bool M16>
+__device__ __forceinline__ void meta_pairs(const unsigned char *from, int kk, __half2 (&y)[2])
 {
-    using S = Stage<BITS, G, M16>;
-    const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     constexpr int HALF = BITS == 2 ? 8 : 4;          // codes in half a word; a pair is (c, c + HALF) of a word
-    float s[4][4];
+    const int lo = 2 * kk / HALF * 2 * HALF + 2 * kk % HALF;
+    if (M16) {
+        const uint32_t a = reinterpret_cast<const uint32_t *>(from)[lo / 2], b = reinterpret_cast<const uint32_t *>(from)[(lo + HALF) / 2];
+        y[0] = as_half2(pair16(a, b, 0));
+        y[1] = as_half2(pair16(a, b, 1));
+    } else {
+        const float2 a = reinterpret_cast<const float2 *>(from)[lo / 2], b = reinterpret_cast<const float2 *>(from)[(lo + HALF) / 2];
+        y[0] = __floats2half2_rn(a.x, b.x);
+        y[1] = __floats2half2_rn(a.y, b.y);
+    }
+}
+template <bool M16>
+__device__ __forceinline__ float meta_at(const unsigned char *from, int i)
+{
+    return M16 ? __half2float(reinterpret_cast<const __half *>(from)[i]) : reinterpret_cast<const float *>(from)[i];
+}
+
+// A step of cached tokens, staged at `st`.
+template <int BITS, bool M16, int NT, bool BF>
+__device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift, const Queries<NT> &queries, float scale_log2, Acc<NT> &acc, Range &range)
+{
+    using S = Stage<BITS, M16>;
+    const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    constexpr int HALF = BITS == 2 ? 8 : 4;
+    float s[NT][2][4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][k][e] = 0.0f;
     {
         const unsigned char *ks = st + S::KS + q * S::QUARTER, *kz = st + S::KZ + q * S::QUARTER;
-        uint32_t s2[16], z2[16];
-        if (!BF) {
-            if (M16) {
-                uint32_t a[16], b[16];
+        uint32_t w[4][BITS];                         // the lane's tokens g, g + 8, g + 16, g + 24
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    *reinterpret_cast<uint4 *>(a + 4 * i) = reinterpret_cast<const uint4 *>(ks)[i];
-                    *reinterpret_cast<uint4 *>(b + 4 * i) = reinterpret_cast<const uint4 *>(kz)[i];
-                }
-#pragma unroll
-                for (int m = 0; m < 16; ++m) {
-                    const int lo = m / HALF * 2 * HALF + m % HALF, hi = lo + HALF;
-                    s2[m] = pair16(a[lo / 2], a[hi / 2], lo);
-                    z2[m] = pair16(b[lo / 2], b[hi / 2], lo);
-                }
-            } else {
-                float a[32], b[32];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    *reinterpret_cast<float4 *>(a + 4 * i) = reinterpret_cast<const float4 *>(ks)[i];
-                    *reinterpret_cast<float4 *>(b + 4 * i) = reinterpret_cast<const float4 *>(kz)[i];
-                }
-#pragma unroll
-                for (int m = 0; m < 16; ++m) {
-                    const int lo = m / HALF * 2 * HALF + m % HALF, hi = lo + HALF;
-                    s2[m] = pack16<false>(a[lo], a[hi]);
-                    z2[m] = pack16<false>(b[lo], b[hi]);
-                }
-            }
-#pragma unroll
-            for (int m = 0; m < 16; ++m) {
-                range.ks = __hmax2(range.ks, __habs2(as_half2(s2[m])));
-                range.kz = __hmax2(range.kz, __habs2(as_half2(z2[m])));
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            uint32_t w[BITS];
-            const unsigned char *from = st + S::KC + (8 * n + g) * S::ROW + q * (S::ROW / 4);
+        for (int e = 0; e < 4; ++e) {
+            const unsigned char *from = st + S::KC + (8 * e + g) * S::ROW + q * (S::ROW / 4);
             if (BITS == 2) {
                 const uint2 v = *reinterpret_cast<const uint2 *>(from);
-                w[0] = v.x; w[1] = v.y;
+                w[e][0] = v.x; w[e][1] = v.y;
             } else {
                 const uint4 v = *reinterpret_cast<const uint4 *>(from);
-                w[0] = v.x; w[1] = v.y; w[BITS - 2] = v.z; w[BITS - 1] = v.w;
+                w[e][0] = v.x; w[e][1] = v.y; w[e][BITS - 2] = v.z; w[e][BITS - 1] = v.w;
             }
-            uint32_t b[16];
+        }
 #pragma unroll
-            for (int m = 0; m < 16; ++m) {
-                if (!BF) {
-                    b[m] = as_u32(__hfma2(code_pair<BITS>(w[m / HALF], m % HALF), as_half2(s2[m]), as_half2(z2[m])));
-                } else {
-                    const int lo = m / HALF * 2 * HALF + m % HALF, hi = lo + HALF;
-                    float y[2];
+        for (int kk = 0; kk < 8; ++kk) {
+            __half2 s2[2], z2[2];
+            if (!BF) {
+                meta_pairs<BITS, M16>(ks, kk, s2);
+                meta_pairs<BITS, M16>(kz, kk, z2);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int c = e ? hi : lo;
-                        const float sc = M16 ? __half2float(reinterpret_cast<const __half *>(ks)[c]) : reinterpret_cast<const float *>(ks)[c];
-                        const float zr = M16 ? __half2float(reinterpret_cast<const __half *>(kz)[c]) : reinterpret_cast<const float *>(kz)[c];
-                        y[e] = fmaf(code_float<BITS>(w[m / HALF], m % HALF + e * HALF), sc, zr);
-                    }
-                    b[m] = pack16<true>(y[0], y[1]);
+                for (int m = 0; m < 2; ++m) {
+                    range.ks = __hmax2(range.ks, __habs2(s2[m]));
+                    range.kz = __hmax2(range.kz, __habs2(z2[m]));
                 }
             }
+            uint32_t b[NT][2];
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) mma16<BF>(s[n], qf[kk], b[2 * kk], b[2 * kk + 1]);
+            for (int t = 0; t < NT; ++t) queries.get(t, kk, b[t]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t a[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {        // token g or g + 8 of the half, pair 2 kk or 2 kk + 1
+                    const int m = 2 * kk + (e >> 1);
+                    const uint32_t word = w[2 * k + (e & 1)][m / HALF];
+                    if (!BF) {
+                        a[e] = as_u32(__hfma2(code_pair<BITS>(word, m % HALF), s2[e >> 1], z2[e >> 1]));
+                    } else {
+                        const int lo = m / HALF * 2 * HALF + m % HALF, hi = lo + HALF;
+                        a[e] = pack16<true>(fmaf(code_float<BITS>(word, m % HALF), meta_at<M16>(ks, lo), meta_at<M16>(kz, lo)),
+                                            fmaf(code_float<BITS>(word, m % HALF + HALF), meta_at<M16>(ks, hi), meta_at<M16>(kz, hi)));
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16<BF>(s[t][k], a, b[t][0], b[t][1]);
+            }
         }
     }
-    uint32_t pa[2][4];
-    softmax_step<BF>(acc, s, scale_log2, pa);
+    uint32_t pb[NT][2][2];
+    softmax_step<NT, BF>(acc, s, scale_log2, pb);
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int k = 0; k < 2; ++k) {
         uint32_t w[4][BITS / 2];                     // 16 channels of the lane's four tokens
         float sc[4], zr[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int t = 16 * kt + 2 * q + (j & 1) + 8 * (j >> 1);
+            const int t = 16 * k + 2 * q + (j & 1) + 8 * (j >> 1);
             const unsigned char *from = st + S::VC + t * S::ROW + g * (S::ROW / 8);
             if (BITS == 2) w[j][0] = *reinterpret_cast<const uint32_t *>(from);
             else {
                 const uint2 v = *reinterpret_cast<const uint2 *>(from);
                 w[j][0] = v.x; w[j][BITS / 2 - 1] = v.y;
             }
-            const int at = t * S::NG + g * 16 / G;
-            sc[j] = M16 ? __half2float(reinterpret_cast<const __half *>(st + S::VS)[at]) : reinterpret_cast<const float *>(st + S::VS)[at];
-            zr[j] = M16 ? __half2float(reinterpret_cast<const __half *>(st + S::VZ)[at]) : reinterpret_cast<const float *>(st + S::VZ)[at];
+            const int at = (t * D + 16 * g) >> g_shift;
+            sc[j] = meta_at<M16>(st + S::VS, at);
+            zr[j] = meta_at<M16>(st + S::VZ, at);
         }
         __half2 s2[2], z2[2];
         uint32_t both[2][BITS];                      // halves of the words of two tokens
@@ -215,71 +266,87 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, const uint3
             }
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            uint32_t b[2];
+        for (int i = 0; i < 8; ++i) {
+            uint32_t a[4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (!BF) b[e] = as_u32(__hfma2(code_pair<BITS>(both[e][i / HALF], i % HALF), s2[e], z2[e]));
+            for (int e = 0; e < 4; ++e) {            // tokens 2 q, 2 q + 1 or the later two (e >> 1), channel i or i + 8 (e & 1)
+                const int c = i + 8 * (e & 1), j = e >> 1;
+                if (!BF) a[e] = as_u32(__hfma2(code_pair<BITS>(both[j][c / HALF], c % HALF), s2[j], z2[j]));
                 else {
                     constexpr int PER = 2 * HALF;
-                    b[e] = pack16<true>(fmaf(code_float<BITS>(w[2 * e][i / PER], i % PER), sc[2 * e], zr[2 * e]),
-                                        fmaf(code_float<BITS>(w[2 * e + 1][i / PER], i % PER), sc[2 * e + 1], zr[2 * e + 1]));
+                    a[e] = pack16<true>(fmaf(code_float<BITS>(w[2 * j][c / PER], c % PER), sc[2 * j], zr[2 * j]),
+                                        fmaf(code_float<BITS>(w[2 * j + 1][c / PER], c % PER), sc[2 * j + 1], zr[2 * j + 1]));
                 }
             }
-            mma16<BF>(acc.o[i], pa[kt], b[0], b[1]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16<BF>(acc.o[t][i], a, pb[t][k][0], pb[t][k][1]);
         }
     }
 }
 
-// A step of rows in full precision: rows u0 .. u0 + 31 of the sequence, of which row g of the item sees the first sees[0], row
-// g + 8 the first sees[1], and none more than `most`.
-template <int BITS, bool BF>
-__device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &sq, int h, int u0, int most, const int (&sees)[2],
-                                          const uint32_t (&qf)[8][4], Acc &acc, Range &range)
+// A step of rows in full precision: rows u0 .. u0 + 31 of the sequence, none from `most` on; row (t, r) of the lane sees the first
+// sees[t][r].
+template <int BITS, int NT, bool BF>
+__device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &sq, int h, int u0, int most, const int (&sees)[NT][2],
+                                       const Queries<NT> &queries, Acc<NT> &acc, Range &range)
 {
     constexpr int HALF = BITS == 2 ? 8 : 4;
     const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    float s[4][4];
+    float s[NT][2][4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        const int u = u0 + 8 * n + g;
-        uint32_t x[16];
+    for (int k = 0; k < 2; ++k) {
+        uint32_t x[2][16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (u < most) v = ldg128(p.k_new + (long long)(sq.k0 + u) * p.knt + (long long)h * p.knh + 32 * q + 8 * i);
-            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
-        }
+        for (int e = 0; e < 2; ++e) {
+            const int u = u0 + 16 * k + 8 * e + g;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = 0.0f;
-        if (!BF)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {            // infinities and NaN are the same in either type
-                const float lo = fabsf(bf16lo_to_f32(x[i])), hi = fabsf(bf16hi_to_f32(x[i]));
-                range.k = fmaxf(range.k, fmaxf(lo < INFINITY ? lo : 0.0f, hi < INFINITY ? hi : 0.0f));
+            for (int i = 0; i < 4; ++i) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (u < most) v = ldg128(p.k_new + (long long)(sq.k0 + u) * p.knt + (long long)h * p.knh + 32 * q + 8 * i);
+                x[e][4 * i] = v.x; x[e][4 * i + 1] = v.y; x[e][4 * i + 2] = v.z; x[e][4 * i + 3] = v.w;
             }
-        uint32_t b[16];
+            if (!BF)
 #pragma unroll
-        for (int m = 0; m < 16; ++m) {
-            const int lo = m / HALF * 2 * HALF + m % HALF;
-            b[m] = pair16(x[lo / 2], x[(lo + HALF) / 2], lo);
-            if (!BF) b[m] = bf16_pair_to_f16(b[m]);
+                for (int i = 0; i < 16; ++i) {        // infinities and NaN are the same in either type
+                    const float lo = fabsf(bf16lo_to_f32(x[e][i])), hi = fabsf(bf16hi_to_f32(x[e][i]));
+                    range.k = fmaxf(range.k, fmaxf(lo < INFINITY ? lo : 0.0f, hi < INFINITY ? hi : 0.0f));
+                }
         }
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) mma16<BF>(s[n], qf[kk], b[2 * kk], b[2 * kk + 1]);
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (u0 + 8 * n + 2 * q + (e & 1) >= sees[e >> 1]) s[n][e] = -INFINITY;
+            for (int e = 0; e < 4; ++e) s[t][k][e] = 0.0f;
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+            uint32_t a[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int m = 2 * kk + (e >> 1), lo = m / HALF * 2 * HALF + m % HALF;
+                a[e] = pair16(x[e & 1][lo / 2], x[e & 1][(lo + HALF) / 2], lo);
+                if (!BF) a[e] = bf16_pair_to_f16(a[e]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                uint32_t b[2];
+                queries.get(t, kk, b);
+                mma16<BF>(s[t][k], a, b[0], b[1]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (u0 + 16 * k + g + 8 * (e >> 1) >= sees[t][e & 1]) s[t][k][e] = -INFINITY;
     }
-    uint32_t pa[2][4];
-    softmax_step<BF>(acc, s, p.scale_log2, pa);
+    uint32_t pb[NT][2][2];
+    softmax_step<NT, BF>(acc, s, p.scale_log2, pb);
     bool odd = false;                                // an infinity or NaN among the lane's values
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int k = 0; k < 2; ++k) {
         uint32_t w[4][8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int u = u0 + 16 * kt + 2 * q + (j & 1) + 8 * (j >> 1);
+            const int u = u0 + 16 * k + 2 * q + (j & 1) + 8 * (j >> 1);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 uint4 v = make_uint4(0, 0, 0, 0);
@@ -297,24 +364,31 @@ __device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &
             }
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            uint32_t b0 = pair16(w[0][i / 2], w[1][i / 2], i), b1 = pair16(w[2][i / 2], w[3][i / 2], i);
-            if (!BF) { b0 = bf16_pair_to_f16(b0); b1 = bf16_pair_to_f16(b1); }
-            mma16<BF>(acc.o[i], pa[kt], b0, b1);
+        for (int i = 0; i < 8; ++i) {
+            uint32_t a[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = i + 8 * (e & 1), j = e >> 1;
+                a[e] = pair16(w[2 * j][c / 2], w[2 * j + 1][c / 2], c);
+                if (!BF) a[e] = bf16_pair_to_f16(a[e]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16<BF>(acc.o[t][i], a, pb[t][k][0], pb[t][k][1]);
         }
     }
     if (__any_sync(0xffffffffu, odd)) {              // rare: the rows that see such a value get it
 #pragma unroll 1
         for (int u = u0; u < min(u0 + STEP, most); ++u) {
-            const __nv_bfloat16 *v = p.v_new + (long long)(sq.k0 + u) * p.vnt + (long long)h * p.vnh + 32 * q;
+            const __nv_bfloat16 *v = p.v_new + (long long)(sq.k0 + u) * p.vnt + (long long)h * p.vnh + 16 * g;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 8; ++i) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float x = __bfloat162float(v[16 * e + i]);
+                for (int e = 0; e < 4; ++e) {        // row e & 1, channel i + 8 (e >> 1)
+                    const float x = __bfloat162float(v[i + 8 * (e >> 1)]);
                     if (fabsf(x) < INFINITY) continue;
-                    if (u < sees[0]) acc.o[i][e] += x;
-                    if (u < sees[1]) acc.o[i][2 + e] += x;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        if (u < sees[t][e & 1]) acc.o[t][i][e] += x;
                 }
             }
         }
@@ -322,28 +396,30 @@ __device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &
 }
 
 // Tiles [ta, tb) of an item by one warp: 32 tokens of every tile.  Returns whether binary16 was too narrow.
-template <int BITS, int G, bool M16, bool BF>
-__device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPlace &pl, const ChunkSeq &sq, int ta, int tb, unsigned char *stages, Acc &acc)
+template <int BITS, bool M16, int NT, bool BF>
+__device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPlace &pl, const ChunkSeq &sq, int ta, int tb, unsigned char *stages, uint32_t *q_sm, Acc<NT> &acc)
 {
-    using S = Stage<BITS, G, M16>;
-    constexpr int HALF = BITS == 2 ? 8 : 4;
+    using S = Stage<BITS, M16>;
+    constexpr int HALF = BITS == 2 ? 8 : 4, R = 8 * NT;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-    const int rows = sq.nq * p.qpk, row0 = pl.qt * R;
+    const int rows = sq.nq * p.qpk, row0 = pl.qt * R, g_shift = 31 - __clz(p.G);
     const int ct = (sq.cached + CHUNK_TILE - 1) / CHUNK_TILE;
     Range range = {};
-    acc.m[0] = acc.m[1] = -INFINITY;
-    acc.l[0] = acc.l[1] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int t = 0; t < NT; ++t) {
+        acc.m[t][0] = acc.m[t][1] = -INFINITY;
+        acc.l[t][0] = acc.l[t][1] = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc.o[i][e] = 0.0f;
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc.o[t][i][e] = 0.0f;
+    }
 
     // ---- the cached steps of this warp: tile ta + i, tokens 32 warp .. of it
     const int c_end = min(tb, ct);
     int steps = max(c_end - ta, 0);
     if (steps > 0 && (c_end - 1) * CHUNK_TILE + STEP * warp >= sq.cached) --steps;           // the last tile may end before this warp's tokens
-    int page_off = 0;                                // lane i: where step (32 b + i)'s tokens are
-    long long page_tok = 0;
+    long long page_tok = 0;                          // lane i: where the tokens of step 32 b + i are
     auto look_up = [&](int first) {
         const int i = first + lane;
         if (i < steps) {
@@ -353,15 +429,14 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
                 atomicOr(p.status, SQUAT_FLAG_PAGES);
                 page = 0;
             }
-            page_off = t - at * p.pool.page_tokens;
-            page_tok = (long long)page * p.pool.page_stride + (long long)pl.h * p.pool.head_stride + page_off;
+            page_tok = (long long)page * p.pool.page_stride + (long long)pl.h * p.pool.head_stride + (t - at * p.pool.page_tokens);
         }
     };
     const unsigned stage0 = smem_u32(stages);
     auto load = [&](int i) {                         // step i into its stage
         if (i < steps) {
             const long long tok = __shfl_sync(0xffffffffu, page_tok, i & 31);
-            const unsigned dst = stage0 + i % S::STAGES * S::BYTES;
+            const unsigned dst = stage0 + i % STAGES * S::BYTES;
             const unsigned char *kc = p.pool.kc + tok * S::ROW, *vc = p.pool.vc + tok * S::ROW;
 #pragma unroll
             for (int j = 0; j < BITS; ++j) {
@@ -369,7 +444,7 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
                 cp16(dst + S::VC + (32 * j + lane) * 16, vc + (32 * j + lane) * 16);
             }
             constexpr int KP = D * S::MS / 16, PER_Q = KP / 4;        // pieces of a row of key metadata, and of a quarter
-            const unsigned char *ks = static_cast<const unsigned char *>(p.pool.ks) + tok / G * (D * S::MS), *kz = static_cast<const unsigned char *>(p.pool.kz) + tok / G * (D * S::MS);
+            const unsigned char *ks = static_cast<const unsigned char *>(p.pool.ks) + (tok >> g_shift) * (D * S::MS), *kz = static_cast<const unsigned char *>(p.pool.kz) + (tok >> g_shift) * (D * S::MS);
             if (M16) {
                 const int j = lane % KP;
                 cp16(dst + (lane < KP ? S::KS : S::KZ) + j / PER_Q * S::QUARTER + j % PER_Q * 16, (lane < KP ? ks : kz) + j * 16);
@@ -377,14 +452,11 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
                 cp16(dst + S::KS + lane / PER_Q * S::QUARTER + lane % PER_Q * 16, ks + lane * 16);
                 cp16(dst + S::KZ + lane / PER_Q * S::QUARTER + lane % PER_Q * 16, kz + lane * 16);
             }
-            constexpr int VP = STEP * S::NG * S::MS / 16;             // pieces of the value scales: 4 .. 32
-            const unsigned char *vs = static_cast<const unsigned char *>(p.pool.vs) + tok * (S::NG * S::MS), *vz = static_cast<const unsigned char *>(p.pool.vz) + tok * (S::NG * S::MS);
-            if (VP == 32) {
+            const int ng = D >> g_shift;                              // value groups of a token: 1, 2 or 4
+            if (lane < 2 * S::MS * ng) {                              // 16-byte pieces of 32 tokens' scales
+                const unsigned char *vs = static_cast<const unsigned char *>(p.pool.vs) + tok * (ng * S::MS), *vz = static_cast<const unsigned char *>(p.pool.vz) + tok * (ng * S::MS);
                 cp16(dst + S::VS + lane * 16, vs + lane * 16);
                 cp16(dst + S::VZ + lane * 16, vz + lane * 16);
-            } else if (lane < 2 * VP) {
-                const int j = lane % VP;
-                cp16(dst + (lane < VP ? S::VS : S::VZ) + j * 16, (lane < VP ? vs : vz) + j * 16);
             }
         }
         cp_commit();
@@ -392,15 +464,16 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
     if (steps > 0) {
         look_up(0);
 #pragma unroll
-        for (int i = 0; i < S::STAGES - 1; ++i) load(i);
+        for (int i = 0; i < STAGES - 1; ++i) load(i);
     }
 
-    // ---- queries: rows g and g + 8, channels 32 q .. + 31, in the order of the key operand
-    uint32_t qf[8][4];
+    // ---- queries: rows 8 t + g, channels 32 q .. + 31, in the order of the key operand
+    Queries<NT> queries;
+    queries.smem = q_sm + 4 * lane;
     float q_max = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int r = row0 + g + 8 * e;
+    for (int t = 0; t < NT; ++t) {
+        const int r = row0 + 8 * t + g;
         uint32_t x[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -408,43 +481,49 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
             if (r < rows) v = ldg128(p.q + (long long)(sq.q0 + r / p.qpk) * p.qt + (long long)(pl.h * p.qpk + r % p.qpk) * p.qh + 32 * q + 8 * i);
             x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
         }
+        uint32_t y[16];
 #pragma unroll
         for (int m = 0; m < 16; ++m) {
             const int lo = m / HALF * 2 * HALF + m % HALF;
-            uint32_t v = pair16(x[lo / 2], x[(lo + HALF) / 2], lo);
+            y[m] = pair16(x[lo / 2], x[(lo + HALF) / 2], lo);
             if (!BF) {
-                q_max = fmaxf(q_max, fmaxf(fabsf(bf16lo_to_f32(v)), fabsf(bf16hi_to_f32(v))));
-                v = bf16_pair_to_f16(v);
+                q_max = fmaxf(q_max, fmaxf(fabsf(bf16lo_to_f32(y[m])), fabsf(bf16hi_to_f32(y[m]))));
+                y[m] = bf16_pair_to_f16(y[m]);
             }
-            qf[m / 2][(m & 1) * 2 + e] = v;
         }
+        queries.put(t, y);
     }
 
 #pragma unroll 1
     for (int i = 0; i < steps; ++i) {
-        cp_wait<S::STAGES - 2>();
+        cp_wait<STAGES - 2>();
         __syncwarp();
-        cached_step<BITS, G, M16, BF>(stages + i % S::STAGES * S::BYTES, qf, p.scale_log2, acc, range);
+        cached_step<BITS, M16, NT, BF>(stages + i % STAGES * S::BYTES, g_shift, queries, p.scale_log2, acc, range);
         __syncwarp();
-        if ((i + S::STAGES - 1) % 32 == 0) look_up(i + S::STAGES - 1);
-        load(i + S::STAGES - 1);
+        if ((i + STAGES - 1) % 32 == 0) look_up(i + STAGES - 1);
+        load(i + STAGES - 1);
     }
     cp_wait<0>();
     __syncwarp();
 
-    // ---- rows in full precision
-    const int last = min(rows, row0 + R) - 1, most = chunk_sees(p, sq, last / p.qpk);
-    const int sees[2] = {chunk_sees(p, sq, min(row0 + g, last) / p.qpk), chunk_sees(p, sq, min(row0 + g + 8, last) / p.qpk)};
+    // ---- rows in full precision, first by the warps that the last cached tile left without tokens
+    const int last = min(rows, row0 + R) - 1, most = chunk_sees(p, sq, last / p.qpk), mine = (warp - sq.cached / STEP) & 3;
+    int sees[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) sees[t][r] = chunk_sees(p, sq, min(row0 + 8 * t + 2 * q + r, last) / p.qpk);
 #pragma unroll 1
     for (int t = max(ta, ct); t < tb; ++t) {
-        const int u0 = (t - ct) * CHUNK_TILE + STEP * warp;
-        if (u0 < most) full_step<BITS, BF>(p, sq, pl.h, u0, most, sees, qf, acc, range);
+        const int u0 = (t - ct) * CHUNK_TILE + STEP * mine;
+        if (u0 < most) full_step<BITS, NT, BF>(p, sq, pl.h, u0, most, sees, queries, acc, range);
     }
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        acc.l[r] += __shfl_xor_sync(0xffffffffu, acc.l[r], 1);
-        acc.l[r] += __shfl_xor_sync(0xffffffffu, acc.l[r], 2);
-    }
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) acc.l[t][r] += __shfl_xor_sync(0xffffffffu, acc.l[t][r], o);
     if (BF) return false;
     constexpr float L = float((1 << BITS) - 1);
     auto top = [](__half2 x) { const float2 f = __half22float2(x); return fmaxf(f.x, f.y); };
@@ -455,10 +534,11 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
     return __any_sync(0xffffffffu, wide) || (!__any_sync(0xffffffffu, v_low >= 0x1p-8f) && __any_sync(0xffffffffu, v_low > 0.0f));
 }
 
-template <int BITS, int G, bool M16>
-__global__ void __launch_bounds__(THREADS, 2) chunk_rows_kernel(const __grid_constant__ ChunkParams params)
+template <int BITS, bool M16, int NT>
+__global__ void __launch_bounds__(THREADS, CTAS<NT>) chunk_rows_kernel(const __grid_constant__ ChunkParams params)
 {
-    using S = Stage<BITS, G, M16>;
+    using S = Stage<BITS, M16>;
+    constexpr int R = 8 * NT;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ ChunkShared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
@@ -471,53 +551,60 @@ __global__ void __launch_bounds__(THREADS, 2) chunk_rows_kernel(const __grid_con
     const long long end = min(at + per, total);
     ChunkPlace pl = chunk_locate<R>(p, sh, at);
     ChunkSeq sq = chunk_seq(p, pl.seq);
+    unsigned char *stages = smem + warp * STAGES * S::BYTES;
+    uint32_t *q_sm = reinterpret_cast<uint32_t *>(smem + WARPS * STAGES * S::BYTES + warp * Queries<NT>::BYTES);
     float *o_sm = reinterpret_cast<float *>(smem), *ml_sm = o_sm + WARPS * R * MERGE_ROW;
     while (at < end) {
-        const int tiles = chunk_tiles<R>(p, sq, pl.qt), ta = pl.tile, tb = (int)min((long long)tiles, ta + (end - at));
-        Acc acc;
-        const bool narrow = run_segment<BITS, G, M16, false>(p, pl, sq, ta, tb, smem + warp * S::STAGES * S::BYTES, acc);
-        if (__syncthreads_or(narrow)) run_segment<BITS, G, M16, true>(p, pl, sq, ta, tb, smem + warp * S::STAGES * S::BYTES, acc);
-        __syncthreads();                             // the stages become the place where the warps meet
+        const int tiles = chunk_tiles<R>(p, sq, pl.qt), begin = pl.at, stop = (int)min((long long)p.start + tiles, begin + (end - at));
+        const int ta = max(begin - p.start, 0), tb = max(stop - p.start, 0);
+        if (ta < tb) {
+            Acc<NT> acc;
+            const bool narrow = run_segment<BITS, M16, NT, false>(p, pl, sq, ta, tb, stages, q_sm, acc);
+            if (__syncthreads_or(narrow)) run_segment<BITS, M16, NT, true>(p, pl, sq, ta, tb, stages, q_sm, acc);
+            __syncthreads();                         // the stages become the place where the warps meet
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float *row = o_sm + (warp * R + g + 8 * e) * MERGE_ROW + 32 * q;
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                *reinterpret_cast<float4 *>(row + 4 * j) = make_float4(acc.o[4 * j][2 * e], acc.o[4 * j + 1][2 * e], acc.o[4 * j + 2][2 * e], acc.o[4 * j + 3][2 * e]);
-                *reinterpret_cast<float4 *>(row + 16 + 4 * j) = make_float4(acc.o[4 * j][2 * e + 1], acc.o[4 * j + 1][2 * e + 1], acc.o[4 * j + 2][2 * e + 1], acc.o[4 * j + 3][2 * e + 1]);
-            }
-            if (q == 0) {
-                ml_sm[(warp * R + g + 8 * e) * 2] = acc.m[e];
-                ml_sm[(warp * R + g + 8 * e) * 2 + 1] = acc.l[e];
-            }
-        }
-        __syncthreads();
-        const bool whole = ta == 0 && tb == tiles;
-        const int row0 = pl.qt * R, n_rows = min(R, sq.nq * p.qpk - row0);
-        const long long slot = 2LL * blockIdx.x + (ta == 0 ? 1 : 0);
+                for (int r = 0; r < 2; ++r) {
+                    float *row = o_sm + (warp * R + 8 * t + 2 * q + r) * MERGE_ROW + 16 * g;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            *reinterpret_cast<float4 *>(row + 8 * e + 4 * i) = make_float4(acc.o[t][4 * i][2 * e + r], acc.o[t][4 * i + 1][2 * e + r], acc.o[t][4 * i + 2][2 * e + r], acc.o[t][4 * i + 3][2 * e + r]);
+                    if (g == 0) {
+                        ml_sm[(warp * R + 8 * t + 2 * q + r) * 2] = acc.m[t][r];
+                        ml_sm[(warp * R + 8 * t + 2 * q + r) * 2 + 1] = acc.l[t][r];
+                    }
+                }
+            __syncthreads();
+            const bool whole = ta == 0 && tb == tiles;
+            const int row0 = pl.qt * R, n_rows = min(R, sq.nq * p.qpk - row0);
+            const long long slot = 2LL * blockIdx.x + (ta == 0 ? 1 : 0);
 #pragma unroll 1
-        for (int r = 0; r < n_rows; ++r) {
-            float m = -INFINITY, l = 0.0f, o = 0.0f;
+            for (int r = 0; r < n_rows; ++r) {
+                float m = -INFINITY, l = 0.0f, o = 0.0f;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) m = max_nan(m, ml_sm[(w * R + r) * 2]);
-            const float use = m == -INFINITY ? 0.0f : m;
+                for (int w = 0; w < WARPS; ++w) m = max_nan(m, ml_sm[(w * R + r) * 2]);
+                const float use = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                const float f = exp2_fast(ml_sm[(w * R + r) * 2] - use);
-                l = fmaf(f, ml_sm[(w * R + r) * 2 + 1], l);
-                o = fmaf(f, o_sm[(w * R + r) * MERGE_ROW + tid], o);
+                for (int w = 0; w < WARPS; ++w) {
+                    const float f = exp2_fast(ml_sm[(w * R + r) * 2] - use);
+                    l = fmaf(f, ml_sm[(w * R + r) * 2 + 1], l);
+                    o = fmaf(f, o_sm[(w * R + r) * MERGE_ROW + tid], o);
+                }
+                if (whole) {
+                    const int row = row0 + r, j = sq.q0 + row / p.qpk, hq = pl.h * p.qpk + row % p.qpk;
+                    p.out[(long long)j * p.ot + (long long)hq * p.oh + tid] = __float2bfloat16_rn(l == 0.0f ? 0.0f : o / l);
+                    if (p.lse && tid == 0) p.lse[(long long)j * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
+                } else {
+                    p.part[(slot * R + r) * D + tid] = o;
+                    if (tid == 0) *reinterpret_cast<float2 *>(p.ml + (slot * R + r) * 2) = make_float2(m, l);
+                }
             }
-            if (whole) {
-                const int row = row0 + r, j = sq.q0 + row / p.qpk, hq = pl.h * p.qpk + row % p.qpk;
-                p.out[(long long)j * p.ot + (long long)hq * p.oh + tid] = __float2bfloat16_rn(l == 0.0f ? 0.0f : o / l);
-                if (p.lse && tid == 0) p.lse[(long long)j * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
-            } else {
-                p.part[(slot * R + r) * D + tid] = o;
-                if (tid == 0) *reinterpret_cast<float2 *>(p.ml + (slot * R + r) * 2) = make_float2(m, l);
-            }
+            __syncthreads();
         }
-        __syncthreads();
-        at += tb - ta;
+        at += stop - begin;
         if (at < end) chunk_next<R>(p, pl, sq);
     }
 }
@@ -535,8 +622,8 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
     const long long c = blockIdx.x, border = (c + 1) * per;
     if (border >= total) return;
     const ChunkPlace pl = chunk_locate<ROWS>(p, sh, border);
-    const long long first = border - pl.tile;        // the item's first tile
-    if (pl.tile == 0 || first < c * per) return;
+    const long long first = border - pl.at + p.start;        // place of the item's first tile
+    if (first >= border || first < c * per) return;
     const ChunkSeq sq = chunk_seq(p, pl.seq);
     const long long parts = (first + chunk_tiles<ROWS>(p, sq, pl.qt) - 1) / per - c + 1;
     const int row0 = pl.qt * ROWS, n_rows = min(ROWS, sq.nq * p.qpk - row0);
@@ -577,47 +664,41 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
     }
 }
 
-template <int BITS, int G, bool M16>
+template <int BITS, bool M16, int NT>
 int launch_rows(const ChunkParams &p, cudaStream_t st)
 {
-    using S = Stage<BITS, G, M16>;
-    constexpr size_t smem = WARPS * S::STAGES * S::BYTES > MERGE_BYTES ? WARPS * S::STAGES * S::BYTES : MERGE_BYTES;
+    using S = Stage<BITS, M16>;
+    constexpr size_t steps = WARPS * (STAGES * S::BYTES + Queries<NT>::BYTES), smem = steps > MERGE_BYTES<NT> ? steps : MERGE_BYTES<NT>;
     static std::atomic<unsigned long long> allowed{0};
-    const int rc = squat_allow_smem(reinterpret_cast<const void *>(chunk_rows_kernel<BITS, G, M16>), smem, allowed);
+    const int rc = squat_allow_smem(reinterpret_cast<const void *>(chunk_rows_kernel<BITS, M16, NT>), smem, allowed);
     if (rc != SQUAT_OK) return rc;
-    return squat_launch(chunk_rows_kernel<BITS, G, M16>, p.n_cta, THREADS, smem, st, p);
+    return squat_launch(chunk_rows_kernel<BITS, M16, NT>, p.n_cta, THREADS, smem, st, p);
 }
-
-}  // namespace
-
-int squat_launch_chunk_rows(const ChunkParams &p, int bits, int meta16, cudaStream_t st)
+template <int NT>
+int launch_rows_tiles(const ChunkParams &p, int bits, int meta16, cudaStream_t st)
 {
-#define SQ_C(BB, GG) return meta16 ? launch_rows<BB, GG, true>(p, st) : launch_rows<BB, GG, false>(p, st)
-    if (bits == 2) { if (p.G == 32) SQ_C(2, 32); if (p.G == 64) SQ_C(2, 64); SQ_C(2, 128); }
-    if (p.G == 32) SQ_C(4, 32);
-    if (p.G == 64) SQ_C(4, 64);
-    SQ_C(4, 128);
-#undef SQ_C
+    if (bits == 2) return meta16 ? launch_rows<2, true, NT>(p, st) : launch_rows<2, false, NT>(p, st);
+    return meta16 ? launch_rows<4, true, NT>(p, st) : launch_rows<4, false, NT>(p, st);
 }
 
-namespace {
-
-// The kernels of a call: rows of the sequences with at most few_rows rows per KV head go to the kernel for few rows, those of the
-// others to the kernel for many, in tiles of 128 or 256.
+// The kernels of a call.  Sequences with at most few_rows rows per KV head go to the kernel for few rows (8 `eights` of them share an
+// item), the others to the kernel for many, in tiles of 128 or 256.
 struct ChunkKernels {
-    bool rows;
+    int eights;                                      // 0: no kernel for few rows
     int tiles;                                       // 0: no kernel for many rows
 };
-constexpr int FEW_ROWS = 16;
+constexpr int FEW_ROWS = 32;
 
 ChunkKernels kernels_for(long long n_q, long long n_seqs, long long max_q, int qpk)
 {
     ChunkKernels k;
-    const long long most = max_q * qpk;
+    const long long most = max_q * qpk, rows = most <= FEW_ROWS ? most : qpk;
     k.tiles = most <= FEW_ROWS ? 0 : most <= 128 ? 1 : 2;
-    k.rows = k.tiles == 0 || n_q != n_seqs * max_q;  // sequences of one length, all of them in the other kernel
+    k.eights = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
+    if (k.tiles && n_q == n_seqs * max_q) k.eights = 0;      // sequences of one length, all of them in the other kernel
     return k;
 }
+int rows_ctas(int eights) { return squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : eights == 3 ? CTAS<3> : CTAS<4>); }
 int matrix_ctas(int tiles) { return squat_sm_count() * (tiles == 2 ? 1 : 2); }
 size_t part_floats(int n_cta, int rows) { return 2 * (size_t)n_cta * rows * (D + 2); }
 void use_part(ChunkParams &p, float *at, int n_cta, int rows)
@@ -626,16 +707,19 @@ void use_part(ChunkParams &p, float *at, int n_cta, int rows)
     p.part = at;
     p.ml = at + 2 * (size_t)n_cta * rows * D;
 }
+template <int ROWS>
+int launch_combine(const ChunkParams &p, cudaStream_t st)
+{
+    return squat_launch(chunk_combine_kernel<ROWS>, dim3((unsigned)p.n_cta, ROWS >= 16 ? ROWS / 16 : 1), D, 0, st, p);
+}
 
 }  // namespace
 
 size_t squat_chunk_workspace_floats(int n_q, int n_q_heads, int n_kv_heads, int max_q)
 {
     (void)n_q;
-    size_t n = part_floats(2 * squat_sm_count(), CHUNK_ROWS);
-    const int tiles = kernels_for(0, 0, max_q, n_q_heads / n_kv_heads).tiles;
-    if (tiles) n += part_floats(matrix_ctas(tiles), 128 * tiles);
-    return n;
+    const ChunkKernels k = kernels_for(-1, 1, max_q, n_q_heads / n_kv_heads);
+    return part_floats(rows_ctas(k.eights), 8 * k.eights) + (k.tiles ? part_floats(matrix_ctas(k.tiles), 128 * k.tiles) : 0);
 }
 
 int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, float *workspace, int max_q, cudaStream_t st)
@@ -648,21 +732,31 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
     if (!p.status) return SQUAT_ERR_CUDA;
     const ChunkKernels k = kernels_for(p.n_q, p.n_seqs, max_q, p.qpk);
     ChunkParams few = p, many = p;
-    few.min_rows = 1;
-    few.max_rows = k.tiles ? FEW_ROWS : 0x7fffffff;
-    few.min_tiles = 2;
-    use_part(few, workspace, 2 * squat_sm_count(), CHUNK_ROWS);
-    many.min_rows = k.rows ? FEW_ROWS + 1 : 1;
-    many.max_rows = 0x7fffffff;
-    many.min_tiles = 4;
     int rc = SQUAT_OK;
     if (k.tiles) {
-        use_part(many, workspace + part_floats(few.n_cta, CHUNK_ROWS), matrix_ctas(k.tiles), 128 * k.tiles);
+        many.min_rows = k.eights ? FEW_ROWS + 1 : 1;
+        many.max_rows = 0x7fffffff;
+        many.min_tiles = 4;
+        many.start = 2;
+        use_part(many, workspace, matrix_ctas(k.tiles), 128 * k.tiles);
+        workspace += part_floats(many.n_cta, 128 * k.tiles);
         rc = squat_launch_chunk_matrix(many, k.tiles, pool->bits, pool->meta16, st);
     }
-    if (rc == SQUAT_OK && k.rows) rc = squat_launch_chunk_rows(few, pool->bits, pool->meta16, st);
-    if (rc == SQUAT_OK && k.tiles == 1) rc = squat_launch(chunk_combine_kernel<128>, dim3((unsigned)many.n_cta, 8), D, 0, st, many);
-    if (rc == SQUAT_OK && k.tiles == 2) rc = squat_launch(chunk_combine_kernel<256>, dim3((unsigned)many.n_cta, 16), D, 0, st, many);
-    if (rc == SQUAT_OK && k.rows) rc = squat_launch(chunk_combine_kernel<CHUNK_ROWS>, dim3((unsigned)few.n_cta, 1), D, 0, st, few);
+    if (rc == SQUAT_OK && k.eights) {
+        few.min_rows = 1;
+        few.max_rows = k.tiles ? FEW_ROWS : 0x7fffffff;
+        few.min_tiles = 4;
+        few.start = 3;
+        use_part(few, workspace, rows_ctas(k.eights), 8 * k.eights);
+        switch (k.eights) {
+            case 1: rc = launch_rows_tiles<1>(few, pool->bits, pool->meta16, st); break;
+            case 2: rc = launch_rows_tiles<2>(few, pool->bits, pool->meta16, st); break;
+            case 3: rc = launch_rows_tiles<3>(few, pool->bits, pool->meta16, st); break;
+            default: rc = launch_rows_tiles<4>(few, pool->bits, pool->meta16, st); break;
+        }
+    }
+    if (rc == SQUAT_OK && k.tiles) rc = k.tiles == 1 ? launch_combine<128>(many, st) : launch_combine<256>(many, st);
+    if (rc == SQUAT_OK && k.eights)
+        rc = k.eights == 1 ? launch_combine<8>(few, st) : k.eights == 2 ? launch_combine<16>(few, st) : k.eights == 3 ? launch_combine<24>(few, st) : launch_combine<32>(few, st);
     return rc;
 }

@@ -2,11 +2,12 @@
 //
 // An item is (sequence, KV head, R rows), a row being a query of one of the KV head's query heads: row r of a sequence is query
 // r / qpk of head h qpk + r mod qpk.  Its work is tiles of 128 tokens: the sequence's cached tokens, then as many of its
-// rows in full precision as the item's last query sees.  All items' tiles stand in one line, and CTA c takes tiles [c per, (c + 1) per)
-// of it, whatever sequences they belong to: a long sequence among short ones, or a single one, is spread over the GPU
-// without the host knowing a length.  An item that begins and ends within a CTA is finished there; of one that crosses a border,
-// every CTA leaves (sum, maximum, denominator) in the workspace and chunk_combine_kernel adds them up.  A CTA has at most two such
-// parts: of the item that it begins in the middle of (slot 2 c), and of the one it does not finish (slot 2 c + 1).
+// rows in full precision as the item's last query sees.  What an item costs besides (its queries, its first loads, its result) counts
+// as `start` tiles in front of them.  All items stand in one line, and CTA c takes places [c per, (c + 1) per) of it, whatever
+// sequences they belong to: a long sequence among short ones, or a single one, is spread over the GPU without the host knowing
+// a length.  An item that begins and ends within a CTA is finished there; of one that crosses a border, every CTA leaves (sum,
+// maximum, denominator) in the workspace and chunk_combine_kernel adds them up.  A CTA has at most two such parts: of the item
+// that it begins in the middle of (slot 2 c), and of the one that it begins and does not finish (slot 2 c + 1).
 #pragma once
 #include "pages.cuh"
 
@@ -25,7 +26,7 @@ struct ChunkParams {
     long long knt, knh, vnt, vnh;
     float scale_log2;                                // softmax scale / ln 2
     int min_rows, max_rows;                          // the kernel's sequences: those with so many rows
-    int n_cta, min_tiles;                            // CTAs that share the work, and the least that one takes
+    int n_cta, min_tiles, start;                     // CTAs that share the work, the least that one takes, and what an item costs besides its tiles
     float *part, *ml;                                // [2 n_cta][R][D], [2 n_cta][R][2]
     unsigned *status;
 };
@@ -70,20 +71,20 @@ __device__ __forceinline__ long long chunk_head_tiles(const ChunkParams &p, cons
 {
     const int n = chunk_row_tiles<R>(p, s);
     long long sum = 0;
-    for (int qt = 0; qt < n; ++qt) sum += chunk_tiles<R>(p, s, qt);
+    for (int qt = 0; qt < n; ++qt) sum += p.start + chunk_tiles<R>(p, s, qt);
     return sum;
 }
 
-// A place in the line of tiles: item and tile within it.
+// A place in the line: item and place within it.
 struct ChunkPlace {
-    int seq, h, qt, tile;
+    int seq, h, qt, at;
 };
 struct ChunkShared {
     long long sums[33];
     ChunkPlace found;
 };
 
-// All threads of the CTA (a multiple of 32, at most 1024) call this.  per: tiles per CTA, total: of all sequences.
+// All threads of the CTA (a multiple of 32, at most 1024) call this.  per: places per CTA, total: of all sequences.
 template <int R>
 __device__ __forceinline__ void chunk_share(const ChunkParams &p, ChunkShared &sm, long long &per, long long &total)
 {
@@ -98,7 +99,7 @@ __device__ __forceinline__ void chunk_share(const ChunkParams &p, ChunkShared &s
     per = max((total + p.n_cta - 1) / p.n_cta, (long long)p.min_tiles);
     __syncthreads();
 }
-// The item that holds tile `at` of the line (at < total), for all threads.
+// The item that holds place `at` of the line (at < total), for all threads.
 template <int R>
 __device__ __forceinline__ ChunkPlace chunk_locate(const ChunkParams &p, ChunkShared &sm, long long at)
 {
@@ -126,7 +127,7 @@ __device__ __forceinline__ ChunkPlace chunk_locate(const ChunkParams &p, ChunkSh
         if (head > 0 && at >= begin && at < end) {
             long long rest = (at - begin) % head;
             int qt = 0;
-            for (int n; rest >= (n = chunk_tiles<R>(p, s, qt)); ++qt) rest -= n;
+            for (int n; rest >= (n = p.start + chunk_tiles<R>(p, s, qt)); ++qt) rest -= n;
             sm.found = {i, (int)((at - begin) / head), qt, (int)rest};
         }
         for (int w = 0; w < warps; ++w) before += sm.sums[w];
@@ -139,7 +140,7 @@ __device__ __forceinline__ ChunkPlace chunk_locate(const ChunkParams &p, ChunkSh
 template <int R>
 __device__ __forceinline__ void chunk_next(const ChunkParams &p, ChunkPlace &w, ChunkSeq &s)
 {
-    w.tile = 0;
+    w.at = 0;
     if (++w.qt < chunk_row_tiles<R>(p, s)) return;
     w.qt = 0;
     if (++w.h < p.H) return;
@@ -190,6 +191,4 @@ __device__ __forceinline__ uint32_t bf16_pair_to_f16(uint32_t x) { return pack16
 __device__ __forceinline__ bool bf16_pair_not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
 
-constexpr int CHUNK_ROWS = 16;                       // rows of an item in the kernel for few rows
 int squat_launch_chunk_matrix(const ChunkParams &p, int tiles, int bits, int meta16, cudaStream_t st);
-int squat_launch_chunk_rows(const ChunkParams &p, int bits, int meta16, cudaStream_t st);

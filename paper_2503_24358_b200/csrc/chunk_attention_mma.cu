@@ -211,11 +211,12 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
     unsigned kv = 0, turns = 0, segments = 0;        // tiles of tokens, scores of a row tile, and segments so far
 
     while (at < end) {
-        const int tiles = chunk_tiles<S::ROWS>(p, sq, pl.qt), ta = pl.tile, tb = (int)min((long long)tiles, ta + (end - at)), n = tb - ta;
+        const int tiles = chunk_tiles<S::ROWS>(p, sq, pl.qt), begin = pl.at, stop = (int)min((long long)p.start + tiles, begin + (end - at));
+        const int ta = max(begin - p.start, 0), tb = max(stop - p.start, 0), n = tb - ta;
         const int rows = sq.nq * p.qpk, row0 = pl.qt * S::ROWS, n_rows = min(S::ROWS, rows - row0), last = row0 + n_rows - 1;
         const int ct = (sq.cached + T - 1) / T, most = chunk_sees(p, sq, last / p.qpk);
         bool bf = false;
-        for (;;) {
+        while (n > 0) {
             if (tid == 0) {
                 sh.wide = 0;
                 sh.odd_first = 0x7fffffff;
@@ -583,7 +584,7 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
             if (!again) break;
             bf = true;
         }
-        at += n;
+        at += stop - begin;
         if (at < end) chunk_next<S::ROWS>(p, pl, sq);
     }
     tc_fence_before();

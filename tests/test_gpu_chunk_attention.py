@@ -162,10 +162,13 @@ def test_strides_streams_and_a_shared_projection():
 
 
 def test_lengths_and_pages_outside_their_limits():
-    """Flagged, cut to the limits, and the other sequences come out right."""
+    """Flagged, cut to the limits, and the other sequences come out right (to their bounds: where a sum is cut into parts depends on
+    all lengths)."""
     seqs = [(1, 128, 3), (1, 256, 2), (2, 64, 4)]
     b = Batch(23, seqs, 4, 2, 2, 32)
     clean, _ = call(b)
+    ref, _, bound = b.expected()
+    right = lambda out, rows: bool(((out.double() - ref)[rows].abs() <= (bound + 2.0 ** -8 * ref.abs())[rows]).all())  # noqa: E731
     sq.squat_get_device_status()
     for field, i, value in (("cached", 0, 10 ** 9), ("cached", 0, -5), ("cached", 0, 37), ("new_len", 0, 10 ** 6), ("new_start", 0, -9), ("new_len", 0, -1),
                             ("page_table", 0, 10 ** 6), ("page_table", 0, -3)):
@@ -174,12 +177,12 @@ def test_lengths_and_pages_outside_their_limits():
         (t[0] if field == "page_table" else t)[i] = value
         out, _ = call(b)
         assert sq.squat_get_device_status() == sq.FLAG_PAGES
-        assert torch.equal(out[1:], clean[1:])
+        assert right(out, slice(1, None))
         t.copy_(old)
     old = b.q_start.clone()
     b.q_start.copy_(torch.tensor([0, 1, 2, 10 ** 6], dtype=torch.int32))
     out, _ = call(b)
-    assert sq.squat_get_device_status() == sq.FLAG_PAGES and torch.equal(out[:2], clean[:2])
+    assert sq.squat_get_device_status() == sq.FLAG_PAGES and right(out, slice(0, 2))
     b.q_start.copy_(old)
     out, _ = call(b)
     assert sq.squat_get_device_status() == 0 and torch.equal(out, clean)
