@@ -135,6 +135,18 @@ class _CtypesCalls:
     def decode_attention(self, softmax_scale, *args):
         return self._lib.squat_decode_attention_ex(*args[:22], softmax_scale, *args[22:])
 
+    def rope_apply(self, *args):
+        return self._lib.squat_rope_apply(*args)
+
+    def pages_write(self, *args):
+        return self._lib.squat_pages_write(*args)
+
+    def pages_read(self, *args):
+        return self._lib.squat_pages_read(*args)
+
+    def chunk_attention(self, softmax_scale, *args):
+        return self._lib.squat_chunk_attention(*args[:22], softmax_scale, *args[22:])
+
 
 def _entry_points(lib):
     """The calls of a serving loop: the extension module built beside the library for this interpreter, else ctypes."""
@@ -143,7 +155,8 @@ def _entry_points(lib):
     from . import _squatcall
     _squatcall.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.squat_quantize_keys, lib.squat_quantize_keys_m16, lib.squat_quantize_values, lib.squat_quantize_values_m16,
-        lib.squat_dequantize, lib.squat_dequantize_m16, lib.squat_decode_attention_ex)))
+        lib.squat_dequantize, lib.squat_dequantize_m16, lib.squat_decode_attention_ex, lib.squat_rope_apply,
+        lib.squat_pages_write, lib.squat_pages_read, lib.squat_chunk_attention)))
     return _squatcall
 
 
@@ -591,43 +604,50 @@ class RopePlan:
         n = (ctypes.c_int * max(1, len(self.sections)))(*self.sections)
         _check(_load().squat_rope_plan_fill(self.base, self.head_dim, ctypes.addressof(n), len(self.sections),
                                             ctypes.addressof(self._plan)), "squat_rope_plan_fill")
-        self.address = ctypes.addressof(self._plan)
+        self.n_axes, self.address = len(self.sections), ctypes.addressof(self._plan)
+
+
+_NO_ROWS = (None, 0, 0, 0, None, 0, 0)
 
 
 def _rows(x, name):
     """Address and strides of [tokens, heads, d]."""
-    if x.dim() != 3 or (x.stride(2) != 1 and x.shape[2] != 1):
+    strides = x.stride()
+    if len(strides) != 3 or strides[2] != 1:
         raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous last dim")
-    st, sh, _ = x.stride()
-    return _dev(x, name), st, sh
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return x.data_ptr(), strides[0], strides[1]
 
 
 def squat_rope_apply(plan: RopePlan, positions: torch.Tensor, q: torch.Tensor = None, k: torch.Tensor = None,
                      q_out: torch.Tensor = None, k_out: torch.Tensor = None, inverse: bool = False, stream=None):
     """Rotates q [tokens, n_q_heads, d] and / or k [tokens, n_kv_heads, d] by their positions [n_axes, tokens] (int32 or int64; one
     axis may come as [tokens]) into q_out and k_out; without an output tensor in place."""
-    if positions.dtype not in (torch.int32, torch.int64):
-        raise TypeError(f"positions must be int32 or int64, not {positions.dtype}")
+    p_dtype = positions.dtype
+    if p_dtype is not torch.int32 and p_dtype is not torch.int64:
+        raise TypeError(f"positions must be int32 or int64, not {p_dtype}")
     if positions.dim() == 1:
         positions = positions.unsqueeze(0)
     x = q if q is not None else k
     if x is None:
         return
-    T, d = x.shape[0], x.shape[2]
-    if tuple(positions.shape) != (len(plan.sections), T) or (T > 1 and positions.stride(1) != 1):
+    dtype = x.dtype
+    T, _, d = x.shape
+    if positions.shape != (plan.n_axes, T) or (T > 1 and positions.stride(1) != 1):
         raise ValueError("positions must be [n_axes, tokens] with contiguous tokens")
     args = []
     for a, b, name in ((q, q_out, "q"), (k, k_out, "k")):
         if a is None:
-            args += [None, 0, 0, 0, None, 0, 0]
+            args += _NO_ROWS
             continue
-        b = a if b is None else b
-        if a.shape != b.shape or a.dtype != x.dtype or b.dtype != x.dtype or a.shape[0] != T or a.shape[2] != d:
+        shape = a.shape
+        if a.dtype is not dtype or shape[0] != T or shape[2] != d or (b is not None and (b.shape != shape or b.dtype is not dtype)):
             raise ValueError("q, k and their outputs must have one dtype, token count and head_dim, and outputs their input's shape")
-        pa, ta, ha = _rows(a, name)
-        args += [pa, a.shape[1], ta, ha, *_rows(b, name + "_out")]
-    _check(_load().squat_rope_apply(plan.address, _dev(positions, "positions"), positions.dtype == torch.int64, positions.stride(0), T,
-                                    d, _dtype_code(x), 1 if inverse else 0, *args, _stream(stream)), "squat_rope_apply")
+        pa = _rows(a, name)
+        args += (pa[0], shape[1], pa[1], pa[2], *(pa if b is None else _rows(b, name)))
+    _check(_direct().rope_apply(plan.address, _dev(positions, "positions"), p_dtype is torch.int64, positions.stride(0), T, d, _dtype_code(x),
+                                1 if inverse else 0, *args, _stream(stream)), "squat_rope_apply")
 
 
 class PagePool:
@@ -687,22 +707,25 @@ class PagePool:
 
 
 def _int32(t, name, numel):
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != numel:
+    if t.dtype is not torch.int32 or t.numel() != numel or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of {numel} elements")
-    return _dev(t, name)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return t.data_ptr()
 
 
 def _pool_rows(pool, slots, tensors, names):
     """Token count and dtype of the key and value rows that come with `slots`, and their addresses and strides."""
     T = slots.numel() * pool.group_size
+    want = (T, pool.n_kv_heads, pool.head_dim)
     args, dtype = [], None
     for x, name in zip(tensors, names):
         if x is None:
-            args += [None, 0, 0]
+            args += (None, 0, 0)
             continue
-        if tuple(x.shape) != (T, pool.n_kv_heads, pool.head_dim):
+        if x.shape != want:
             raise ValueError(f"{name} must be [len(slots) * group_size, n_kv_heads, head_dim]")
-        if dtype is not None and x.dtype != dtype:
+        if dtype is not None and x.dtype is not dtype:
             raise ValueError(f"{names[0]} and {names[1]} must have one dtype")
         dtype = x.dtype
         args += _rows(x, name)
@@ -722,7 +745,7 @@ def squat_pages_write(pool: PagePool, slots: torch.Tensor, k: torch.Tensor = Non
     if dtype is None:
         return
     x = k if k is not None else v
-    _check(_load().squat_pages_write(None if s is None else s.handle.value, pool.address, _int32(slots, "slots", slots.numel()), T, _dtype_code(x),
+    _check(_direct().pages_write(None if s is None else s.handle.value, pool.address, _int32(slots, "slots", slots.numel()), T, _dtype_code(x),
                                      *args, None if workspace is None else _dev(workspace, "workspace"),
                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
            "squat_pages_write")
@@ -734,7 +757,7 @@ def squat_pages_read(pool: PagePool, slots: torch.Tensor, k_out: torch.Tensor = 
     if dtype is None:
         return
     x = k_out if k_out is not None else v_out
-    _check(_load().squat_pages_read(pool.address, _int32(slots, "slots", slots.numel()), T, _dtype_code(x), *args, _stream(stream)),
+    _check(_direct().pages_read(pool.address, _int32(slots, "slots", slots.numel()), T, _dtype_code(x), *args, _stream(stream)),
            "squat_pages_read")
 
 
@@ -751,29 +774,33 @@ def squat_chunk_attention(q: torch.Tensor, pool: PagePool, q_start: torch.Tensor
     k_new / v_new[new_start[i]:][:new_len[i]] (bfloat16 [rows, n_kv_heads, d]).  Index tensors are int32 on the device and are
     read there; max_q is the largest number of queries of a sequence.  workspace: CUDA uint8 of
     squat_chunk_attention_workspace_bytes(n_q, n_q_heads, n_kv_heads, max_q)."""
-    n_seqs = cached_len.numel()
-    if q.dim() != 3 or q.shape != out.shape or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.shape[2] != pool.head_dim:
+    n_seqs, bf16, shape, d = cached_len.numel(), torch.bfloat16, q.shape, pool.head_dim
+    if len(shape) != 3 or shape != out.shape or q.dtype is not bf16 or out.dtype is not bf16 or shape[2] != d:
         raise ValueError("q and out must be bfloat16 [n_q, n_q_heads, head_dim]")
-    if page_table.dim() != 2 or page_table.shape[0] != n_seqs:
+    table = page_table.shape
+    if len(table) != 2 or table[0] != n_seqs:
         raise ValueError("page_table must be [n_seqs, pages]")
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != shape[:2]):
         raise ValueError("lse must be contiguous float32 [n_q, n_q_heads]")
-    n_new, rows = 0, [None, None, 0, 0, 0, 0, 0]
-    starts = [None, None]
+    rows, starts = (None, None, 0, 0, 0, 0, 0), (None, None)
     if k_new is not None and k_new.shape[0] > 0:
-        if v_new is None or k_new.shape != v_new.shape or k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16 or \
-                tuple(k_new.shape[1:]) != (pool.n_kv_heads, pool.head_dim) or new_start is None or new_len is None:
+        n_new, heads, kd = k_new.shape
+        if v_new is None or v_new.shape != k_new.shape or k_new.dtype is not bf16 or v_new.dtype is not bf16 or heads != pool.n_kv_heads or kd != d or \
+                new_start is None or new_len is None:
             raise ValueError("k_new and v_new must be bfloat16 [rows, n_kv_heads, head_dim], with new_start and new_len")
         (pk, kt, kh), (pv, vt, vh) = _rows(k_new, "k_new"), _rows(v_new, "v_new")
-        rows = [pk, pv, k_new.shape[0], kt, kh, vt, vh]
-        starts = [_int32(new_start, "new_start", n_seqs), _int32(new_len, "new_len", n_seqs)]
-    pq, qt, qh = _rows(q, "q")
-    po, ot, oh = _rows(out, "out")
-    _check(_load().squat_chunk_attention(
-        pq, q.shape[0], q.shape[1], qt, qh, pool.address, n_seqs, _int32(q_start, "q_start", n_seqs + 1), _int32(cached_len, "cached_len", n_seqs),
-        _int32(page_table, "page_table", page_table.numel()), page_table.shape[1], *rows, *starts, max_q, 1 if causal else 0, softmax_scale,
-        po, ot, oh, None if lse is None else _dev(lse, "lse"), _dev(workspace, "workspace"),
-        workspace.numel() * workspace.element_size(), _stream(stream)), "squat_chunk_attention")
+        rows = (pk, pv, n_new, kt, kh, vt, vh)
+        starts = (_int32(new_start, "new_start", n_seqs), _int32(new_len, "new_len", n_seqs))
+    _check(_direct().chunk_attention(
+        softmax_scale, *_q_rows(q, "q"), pool.address, n_seqs, _int32(q_start, "q_start", n_seqs + 1), _int32(cached_len, "cached_len", n_seqs),
+        _int32(page_table, "page_table", n_seqs * table[1]), table[1], *rows, *starts, max_q, 1 if causal else 0, *_rows(out, "out"),
+        None if lse is None else _dev(lse, "lse"), _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)),
+        "squat_chunk_attention")
+
+
+def _q_rows(q, name):
+    p, st, sh = _rows(q, name)
+    return p, q.shape[0], q.shape[1], st, sh
 
 
 def squat_get_device_status(clear: bool = True, stream=None) -> int:

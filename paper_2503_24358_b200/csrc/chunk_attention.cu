@@ -6,8 +6,8 @@
 // The cache's bytes bound it, if the two instructions that a code costs can be issued meanwhile.  So nothing is staged for
 // the tensor core: the operands of mma.sync m16n8k16 are made in the registers where it wants them, the dequantized ones once for
 // up to 32 rows, 8 rows a product (the tcgen05 form wants them in shared or tensor memory, and 128 rows to fill it).
-//   - A warp takes 32 tokens at a time (they lie in one page and one group of keys) and keeps its own maximum, denominator and
-//     sum; a CTA's warps are joined at the end.
+//   - A warp works by itself: it takes 32 tokens at a time (they lie in one page and one group of keys) of its own share of the work.
+//     (Warps that shared an item waited for one another at its end: a quarter of all stalls.)
 //   - Scores, transposed: tokens are the 16 side.  Lane (g, q) holds tokens g and g + 8, channels 32 q .. 32 q + 31: a contiguous
 //     quarter of their codes.  Which of them stand at which of the steps of the contraction is free, as long as the queries agree: the two
 //     codes 16 bits apart in a word become a pair of binary16 numbers by one logic instruction (their bits under the exponent of 2^(10 - s)
@@ -35,9 +35,6 @@ struct Stage {                                       // one step's part of the c
     static constexpr int KC = 0, VC = STEP * ROW, KS = 2 * STEP * ROW, KZ = KS + 4 * QUARTER, VS = KZ + 4 * QUARTER, VZ = VS + STEP * 4 * MS;
     static constexpr int BYTES = VZ + STEP * 4 * MS;
 };
-constexpr int MERGE_ROW = D + 4;
-template <int NT>
-constexpr int MERGE_BYTES = WARPS * 8 * NT * (MERGE_ROW + 2) * 4;
 template <int NT>
 constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;  // to an SM
 
@@ -67,10 +64,12 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
     return y;
 }
 
-// what a warp has seen of the magnitudes
+// What a lane has seen of the magnitudes.
 struct Range {
-    __half2 ks, kz, vs, vz;                          // quantized scales and zero-points
-    float k, v;                                      // rows in full precision
+    __half2 meta;                                    // largest of the values' scales and zero-points
+    float k, v;                                      // largest finite ones among rows in full precision
+    float score;                                     // largest score of cached tokens
+    int odd_first, odd_last;                         // range of rows in full precision with infinities or NaN among their values
 };
 
 // The other operand of the scores: rows 8 t + g, pairs 2 kk and 2 kk + 1 of the lane's channels.  In registers; with four times eight rows,
@@ -172,7 +171,7 @@ __device__ __forceinline__ float meta_at(const unsigned char *from, int i)
 
 // A step of cached tokens, staged at `st`.
 template <int BITS, bool M16, int NT, bool BF>
-__device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift, const Queries<NT> &queries, float scale_log2, Acc<NT> &acc, Range &range)
+__device__ __forceinline__ void cached_step(const unsigned char *st, const CodeBias<BITS> &bias, int g_shift, const Queries<NT> &queries, float scale_log2, Acc<NT> &acc, Range &range)
 {
     using S = Stage<BITS, M16>;
     const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
@@ -184,7 +183,15 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[t][k][e] = 0.0f;
+    // For few rows it is less to scale the queries than the codes (16 products a row of eight rather than 128 differences and multiply-adds)
+    constexpr bool FOLD = !BF && NT <= 2;
     {
+        float alike[NT][4];
+        if (FOLD)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) alike[t][e] = 0.0f;
         const unsigned char *ks = st + S::KS + q * S::QUARTER, *kz = st + S::KZ + q * S::QUARTER;
         uint32_t w[4][BITS];                         // the lane's tokens g, g + 8, g + 16, g + 24
 #pragma unroll
@@ -204,15 +211,23 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift
             if (!BF) {
                 meta_pairs<BITS, M16>(ks, kk, s2);
                 meta_pairs<BITS, M16>(kz, kk, z2);
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    range.ks = __hmax2(range.ks, __habs2(s2[m]));
-                    range.kz = __hmax2(range.kz, __habs2(z2[m]));
-                }
             }
             uint32_t b[NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) queries.get(t, kk, b[t]);
+            if (FOLD) {
+                // sum q (z + s c) = sum q z - sum (q s) B + sum (q s) (B + c): the first two are the same for every token, so they are
+                // products with rows that are all alike, made once for both halves
+                const uint32_t za[4] = {as_u32(z2[0]), as_u32(z2[0]), as_u32(z2[1]), as_u32(z2[1])};
+                const uint32_t b0 = code_bias<BITS>(2 * kk % HALF) | 0x80008000u, b1 = code_bias<BITS>((2 * kk + 1) % HALF) | 0x80008000u, ba[4] = {b0, b0, b1, b1};
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    mma16<false>(alike[t], za, b[t][0], b[t][1]);
+                    b[t][0] = as_u32(__hmul2(as_half2(b[t][0]), s2[0]));
+                    b[t][1] = as_u32(__hmul2(as_half2(b[t][1]), s2[1]));
+                    mma16<false>(alike[t], ba, b[t][0], b[t][1]);
+                }
+            }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 uint32_t a[4];
@@ -220,8 +235,10 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift
                 for (int e = 0; e < 4; ++e) {        // token g or g + 8 of the half, pair 2 kk or 2 kk + 1
                     const int m = 2 * kk + (e >> 1);
                     const uint32_t word = w[2 * k + (e & 1)][m / HALF];
-                    if (!BF) {
-                        a[e] = as_u32(__hfma2(code_pair<BITS>(word, m % HALF), s2[e >> 1], z2[e >> 1]));
+                    if (FOLD) {
+                        a[e] = bias.biased(word, m % HALF);
+                    } else if (!BF) {
+                        a[e] = as_u32(__hfma2(bias.codes(word, m % HALF), s2[e >> 1], z2[e >> 1]));
                     } else {
                         const int lo = m / HALF * 2 * HALF + m % HALF, hi = lo + HALF;
                         a[e] = pack16<true>(fmaf(code_float<BITS>(word, m % HALF), meta_at<M16>(ks, lo), meta_at<M16>(kz, lo)),
@@ -232,7 +249,21 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift
                 for (int t = 0; t < NT; ++t) mma16<BF>(s[t][k], a, b[t][0], b[t][1]);
             }
         }
+        if (FOLD)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[t][k][e] += alike[t][e & 1];
     }
+    if (!BF)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) range.score = max_nan(range.score, fabsf(s[t][k][e]));
     uint32_t pb[NT][2][2];
     softmax_step<NT, BF>(acc, s, scale_log2, pb);
 #pragma unroll
@@ -259,8 +290,7 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift
             for (int e = 0; e < 2; ++e) {
                 s2[e] = __floats2half2_rn(sc[2 * e], sc[2 * e + 1]);
                 z2[e] = __floats2half2_rn(zr[2 * e], zr[2 * e + 1]);
-                range.vs = __hmax2(range.vs, __habs2(s2[e]));
-                range.vz = __hmax2(range.vz, __habs2(z2[e]));
+                range.meta = __hmax2(range.meta, __hmax2(__habs2(s2[e]), __habs2(z2[e])));
 #pragma unroll
                 for (int i = 0; i < BITS; ++i) both[e][i] = pair16(w[2 * e][i / 2], w[2 * e + 1][i / 2], i);
             }
@@ -271,7 +301,7 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, int g_shift
 #pragma unroll
             for (int e = 0; e < 4; ++e) {            // tokens 2 q, 2 q + 1 or the later two (e >> 1), channel i or i + 8 (e & 1)
                 const int c = i + 8 * (e & 1), j = e >> 1;
-                if (!BF) a[e] = as_u32(__hfma2(code_pair<BITS>(both[j][c / HALF], c % HALF), s2[j], z2[j]));
+                if (!BF) a[e] = as_u32(__hfma2(bias.codes(both[j][c / HALF], c % HALF), s2[j], z2[j]));
                 else {
                     constexpr int PER = 2 * HALF;
                     a[e] = pack16<true>(fmaf(code_float<BITS>(w[2 * j][c / PER], c % PER), sc[2 * j], zr[2 * j]),
@@ -376,35 +406,37 @@ __device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &
             for (int t = 0; t < NT; ++t) mma16<BF>(acc.o[t][i], a, pb[t][k][0], pb[t][k][1]);
         }
     }
-    if (__any_sync(0xffffffffu, odd)) {              // rare: the rows that see such a value get it
-#pragma unroll 1
-        for (int u = u0; u < min(u0 + STEP, most); ++u) {
-            const __nv_bfloat16 *v = p.v_new + (long long)(sq.k0 + u) * p.vnt + (long long)h * p.vnh + 16 * g;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {        // row e & 1, channel i + 8 (e >> 1)
-                    const float x = __bfloat162float(v[i + 8 * (e >> 1)]);
-                    if (fabsf(x) < INFINITY) continue;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-                        if (u < sees[t][e & 1]) acc.o[t][i][e] += x;
-                }
-            }
-        }
+    if (__any_sync(0xffffffffu, odd)) {
+        range.odd_first = min(range.odd_first, u0);
+        range.odd_last = min(u0 + STEP, most) - 1;
     }
 }
 
-// Tiles [ta, tb) of an item by one warp: 32 tokens of every tile.  Returns whether binary16 was too narrow.
+// Rare: infinities and NaN among the values of rows [first, last], which were left out of the products, for the rows that see them.
+template <int NT>
+__device__ __noinline__ void add_not_finite(const __nv_bfloat16 *v0, long long stride, int first, int last, const int *sees, float *o)
+{
+#pragma unroll 1
+    for (int u = first; u <= last; ++u)
+#pragma unroll 1
+        for (int i = 0; i < 32 * NT; ++i) {          // tile of rows i / 32, channel i / 4 mod 8 (or that + 8), row i mod 2 of the lane's
+            const float x = __bfloat162float(v0[u * stride + i / 4 % 8 + 8 * (i >> 1 & 1)]);
+            if (!(fabsf(x) < INFINITY) && u < sees[i / 32 * 2 + (i & 1)]) o[i] += x;
+        }
+}
+
+// Steps [ta, tb) of an item.  Returns whether binary16 was too narrow.
 template <int BITS, bool M16, int NT, bool BF>
-__device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPlace &pl, const ChunkSeq &sq, int ta, int tb, unsigned char *stages, uint32_t *q_sm, Acc<NT> &acc)
+__device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPlace &pl, const ChunkSeq &sq, int ta, int tb, unsigned char *stages, uint32_t *q_sm, Acc<NT> &acc, Range &range)
 {
     using S = Stage<BITS, M16>;
     constexpr int HALF = BITS == 2 ? 8 : 4, R = 8 * NT;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int rows = sq.nq * p.qpk, row0 = pl.qt * R, g_shift = 31 - __clz(p.G);
-    const int ct = (sq.cached + CHUNK_TILE - 1) / CHUNK_TILE;
-    Range range = {};
+    const int ct = sq.cached / STEP;                 // (the group size, and so a length, is a multiple of it)
+    range = {};
+    range.odd_first = 0x7fffffff;
+    range.odd_last = -1;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         acc.m[t][0] = acc.m[t][1] = -INFINITY;
@@ -415,15 +447,13 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
             for (int e = 0; e < 4; ++e) acc.o[t][i][e] = 0.0f;
     }
 
-    // ---- the cached steps of this warp: tile ta + i, tokens 32 warp .. of it
-    const int c_end = min(tb, ct);
-    int steps = max(c_end - ta, 0);
-    if (steps > 0 && (c_end - 1) * CHUNK_TILE + STEP * warp >= sq.cached) --steps;           // the last tile may end before this warp's tokens
+    // ---- cached steps
+    const int steps = max(min(tb, ct) - ta, 0);
     long long page_tok = 0;                          // lane i: where the tokens of step 32 b + i are
     auto look_up = [&](int first) {
         const int i = first + lane;
         if (i < steps) {
-            const int t = (ta + i) * CHUNK_TILE + STEP * warp, at = t / p.pool.page_tokens;
+            const int t = (ta + i) * STEP, at = t / p.pool.page_tokens;
             int page = __ldg(p.page_table + (long long)pl.seq * p.table_stride + at);
             if ((unsigned)page >= (unsigned)p.pool.n_pages) {
                 atomicOr(p.status, SQUAT_FLAG_PAGES);
@@ -494,11 +524,12 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
         queries.put(t, y);
     }
 
+    const CodeBias<BITS> bias;
 #pragma unroll 1
     for (int i = 0; i < steps; ++i) {
         cp_wait<STAGES - 2>();
         __syncwarp();
-        cached_step<BITS, M16, NT, BF>(stages + i % STAGES * S::BYTES, g_shift, queries, p.scale_log2, acc, range);
+        cached_step<BITS, M16, NT, BF>(stages + i % STAGES * S::BYTES, bias, g_shift, queries, p.scale_log2, acc, range);
         __syncwarp();
         if ((i + STAGES - 1) % 32 == 0) look_up(i + STAGES - 1);
         load(i + STAGES - 1);
@@ -506,8 +537,8 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
     cp_wait<0>();
     __syncwarp();
 
-    // ---- rows in full precision, first by the warps that the last cached tile left without tokens
-    const int last = min(rows, row0 + R) - 1, most = chunk_sees(p, sq, last / p.qpk), mine = (warp - sq.cached / STEP) & 3;
+    // ---- rows in full precision
+    const int last = min(rows, row0 + R) - 1, most = chunk_sees(p, sq, last / p.qpk);
     int sees[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -515,7 +546,7 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
         for (int r = 0; r < 2; ++r) sees[t][r] = chunk_sees(p, sq, min(row0 + 8 * t + 2 * q + r, last) / p.qpk);
 #pragma unroll 1
     for (int t = max(ta, ct); t < tb; ++t) {
-        const int u0 = (t - ct) * CHUNK_TILE + STEP * mine;
+        const int u0 = (t - ct) * STEP;
         if (u0 < most) full_step<BITS, NT, BF>(p, sq, pl.h, u0, most, sees, queries, acc, range);
     }
 #pragma unroll
@@ -525,12 +556,17 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) acc.l[t][r] += __shfl_xor_sync(0xffffffffu, acc.l[t][r], o);
     if (BF) return false;
-    constexpr float L = float((1 << BITS) - 1);
-    auto top = [](__half2 x) { const float2 f = __half22float2(x); return fmaxf(f.x, f.y); };
-    // 2^12 for queries and keys: what falls below 2^-25 of binary16 is then less than 2^-13 of a score's unit even in 128 products
-    const float k_top = fmaxf(fmaf(L, top(range.ks), top(range.kz)), range.k), v_top = fmaxf(fmaf(L, top(range.vs), top(range.vz)), range.v);
-    const bool wide = !(q_max < 4096.0f) || !(k_top < 4096.0f) || !(v_top < 65000.0f);
-    const float v_low = fmaxf(fmaxf(top(range.vs), top(range.vz)), range.v);
+    // Dequantized keys and values beyond binary16 have become infinities, and so have scores or sums.  Queries below 2^12: what falls
+    // below 2^-25 of a key's scale or zero-point is then less than 2^-13 of a score's unit even in 128 products.
+    bool wide = !(q_max < 4096.0f) || !(range.k < 65000.0f) || !(range.score < INFINITY);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) wide |= !(fabsf(acc.o[t][i][e]) < INFINITY) && acc.m[t][e & 1] < INFINITY;      // (a row with an infinite score of its own has no sum)
+    const float2 meta = __half22float2(range.meta);
+    const float v_low = fmaxf(fmaxf(meta.x, meta.y), range.v);
     return __any_sync(0xffffffffu, wide) || (!__any_sync(0xffffffffu, v_low >= 0x1p-8f) && __any_sync(0xffffffffu, v_low > 0.0f));
 }
 
@@ -541,76 +577,79 @@ __global__ void __launch_bounds__(THREADS, CTAS<NT>) chunk_rows_kernel(const __g
     constexpr int R = 8 * NT;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ ChunkShared sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
     ChunkParams p = params;
     grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
     long long per, total;
-    chunk_share<R>(p, sh, per, total);
-    long long at = per * blockIdx.x;
-    if (at >= total) return;
+    chunk_share<R, STEP>(p, sh, per, total);
+    const long long worker = (long long)blockIdx.x * WARPS + warp;
+    long long at = per * worker;
+    if (per * blockIdx.x * WARPS >= total) return;
+    chunk_locate<R, STEP, WARPS>(p, sh, per * blockIdx.x * WARPS, per);
+    if (at >= total) return;                         // from here on every warp is by itself
     const long long end = min(at + per, total);
-    ChunkPlace pl = chunk_locate<R>(p, sh, at);
+    ChunkPlace pl = sh.found[warp];
     ChunkSeq sq = chunk_seq(p, pl.seq);
     unsigned char *stages = smem + warp * STAGES * S::BYTES;
     uint32_t *q_sm = reinterpret_cast<uint32_t *>(smem + WARPS * STAGES * S::BYTES + warp * Queries<NT>::BYTES);
-    float *o_sm = reinterpret_cast<float *>(smem), *ml_sm = o_sm + WARPS * R * MERGE_ROW;
     while (at < end) {
-        const int tiles = chunk_tiles<R>(p, sq, pl.qt), begin = pl.at, stop = (int)min((long long)p.start + tiles, begin + (end - at));
+        const int tiles = chunk_tiles<R, STEP>(p, sq, pl.qt), begin = pl.at, stop = (int)min((long long)p.start + tiles, begin + (end - at));
         const int ta = max(begin - p.start, 0), tb = max(stop - p.start, 0);
         if (ta < tb) {
             Acc<NT> acc;
-            const bool narrow = run_segment<BITS, M16, NT, false>(p, pl, sq, ta, tb, stages, q_sm, acc);
-            if (__syncthreads_or(narrow)) run_segment<BITS, M16, NT, true>(p, pl, sq, ta, tb, stages, q_sm, acc);
-            __syncthreads();                         // the stages become the place where the warps meet
+            Range range;
+            if (run_segment<BITS, M16, NT, false>(p, pl, sq, ta, tb, stages, q_sm, acc, range)) run_segment<BITS, M16, NT, true>(p, pl, sq, ta, tb, stages, q_sm, acc, range);
+            const int row0 = pl.qt * R, n_rows = min(R, sq.nq * p.qpk - row0);
+            if (range.odd_first <= range.odd_last) {
+                float o[32 * NT];
+                int sees[2 * NT];
+#pragma unroll
+                for (int i = 0; i < 32 * NT; ++i) o[i] = acc.o[i / 32][i / 4 % 8][i % 4];
+#pragma unroll
+                for (int i = 0; i < 2 * NT; ++i) sees[i] = chunk_sees(p, sq, min(row0 + i / 2 * 8 + 2 * q + i % 2, sq.nq * p.qpk - 1) / p.qpk);
+                add_not_finite<NT>(p.v_new + (long long)sq.k0 * p.vnt + (long long)pl.h * p.vnh + 16 * g, p.vnt, range.odd_first, range.odd_last, sees, o);
+#pragma unroll
+                for (int i = 0; i < 32 * NT; ++i) acc.o[i / 32][i / 4 % 8][i % 4] = o[i];
+            }
+            const bool whole = ta == 0 && tb == tiles;
+            const long long slot = 2 * worker + (ta == 0 ? 1 : 0);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    float *row = o_sm + (warp * R + 8 * t + 2 * q + r) * MERGE_ROW + 16 * g;
+                    const int row = 8 * t + 2 * q + r;
+                    if (row >= n_rows) continue;
+                    float y[16];                     // channels 16 g ..
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
+                    for (int i = 0; i < 16; ++i) y[i] = acc.o[t][i % 8][i / 8 * 2 + r];
+                    const float m = acc.m[t][r], l = acc.l[t][r];
+                    if (whole) {
+                        const int j = sq.q0 + (row0 + row) / p.qpk, hq = pl.h * p.qpk + (row0 + row) % p.qpk;
+                        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                        uint32_t w[8];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            *reinterpret_cast<float4 *>(row + 8 * e + 4 * i) = make_float4(acc.o[t][4 * i][2 * e + r], acc.o[t][4 * i + 1][2 * e + r], acc.o[t][4 * i + 2][2 * e + r], acc.o[t][4 * i + 3][2 * e + r]);
-                    if (g == 0) {
-                        ml_sm[(warp * R + 8 * t + 2 * q + r) * 2] = acc.m[t][r];
-                        ml_sm[(warp * R + 8 * t + 2 * q + r) * 2 + 1] = acc.l[t][r];
+                        for (int i = 0; i < 8; ++i) w[i] = pack16<true>(y[2 * i] * inv, y[2 * i + 1] * inv);
+                        uint4 *to = reinterpret_cast<uint4 *>(p.out + (long long)j * p.ot + (long long)hq * p.oh + 16 * g);
+                        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                        to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+                        if (p.lse && g == 0) p.lse[(long long)j * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
+                    } else {
+                        float4 *to = reinterpret_cast<float4 *>(p.part + (slot * R + row) * D + 16 * g);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                        if (g == 0) *reinterpret_cast<float2 *>(p.ml + (slot * R + row) * 2) = make_float2(m, l);
                     }
                 }
-            __syncthreads();
-            const bool whole = ta == 0 && tb == tiles;
-            const int row0 = pl.qt * R, n_rows = min(R, sq.nq * p.qpk - row0);
-            const long long slot = 2LL * blockIdx.x + (ta == 0 ? 1 : 0);
-#pragma unroll 1
-            for (int r = 0; r < n_rows; ++r) {
-                float m = -INFINITY, l = 0.0f, o = 0.0f;
-#pragma unroll
-                for (int w = 0; w < WARPS; ++w) m = max_nan(m, ml_sm[(w * R + r) * 2]);
-                const float use = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-                for (int w = 0; w < WARPS; ++w) {
-                    const float f = exp2_fast(ml_sm[(w * R + r) * 2] - use);
-                    l = fmaf(f, ml_sm[(w * R + r) * 2 + 1], l);
-                    o = fmaf(f, o_sm[(w * R + r) * MERGE_ROW + tid], o);
-                }
-                if (whole) {
-                    const int row = row0 + r, j = sq.q0 + row / p.qpk, hq = pl.h * p.qpk + row % p.qpk;
-                    p.out[(long long)j * p.ot + (long long)hq * p.oh + tid] = __float2bfloat16_rn(l == 0.0f ? 0.0f : o / l);
-                    if (p.lse && tid == 0) p.lse[(long long)j * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
-                } else {
-                    p.part[(slot * R + r) * D + tid] = o;
-                    if (tid == 0) *reinterpret_cast<float2 *>(p.ml + (slot * R + r) * 2) = make_float2(m, l);
-                }
-            }
-            __syncthreads();
+            __syncwarp();
         }
         at += stop - begin;
         if (at < end) chunk_next<R>(p, pl, sq);
     }
 }
 
-// CTA c: the item that CTA c of the main kernel began and did not finish, if there is one.  A warp takes a row, four channels a lane.
-template <int ROWS>
+// The item that worker c began and did not finish, if there is one.  A warp takes a row at a time, four channels a lane; workers that
+// are CTAs have a CTA (and blockIdx.y) of warps here, workers that are warps a warp.
+template <int ROWS, int U, bool CTA_WORKERS>
 __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant__ ChunkParams params)
 {
     __shared__ ChunkShared sh;
@@ -618,17 +657,21 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
     ChunkParams p = params;
     grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
     long long per, total;
-    chunk_share<ROWS>(p, sh, per, total);
-    const long long c = blockIdx.x, border = (c + 1) * per;
+    chunk_share<ROWS, U>(p, sh, per, total);
+    constexpr int WORKERS = CTA_WORKERS ? 1 : WARPS;
+    const long long c0 = (long long)blockIdx.x * WORKERS, c = c0 + (CTA_WORKERS ? 0 : warp), border = (c + 1) * per;
+    if ((c0 + 1) * per >= total) return;
+    chunk_locate<ROWS, U, WORKERS>(p, sh, (c0 + 1) * per, per);
     if (border >= total) return;
-    const ChunkPlace pl = chunk_locate<ROWS>(p, sh, border);
+    const ChunkPlace pl = sh.found[CTA_WORKERS ? 0 : warp];
     const long long first = border - pl.at + p.start;        // place of the item's first tile
     if (first >= border || first < c * per) return;
     const ChunkSeq sq = chunk_seq(p, pl.seq);
-    const long long parts = (first + chunk_tiles<ROWS>(p, sq, pl.qt) - 1) / per - c + 1;
+    const long long parts = (first + chunk_tiles<ROWS, U>(p, sq, pl.qt) - 1) / per - c + 1;
     const int row0 = pl.qt * ROWS, n_rows = min(ROWS, sq.nq * p.qpk - row0);
+    const int r_first = CTA_WORKERS ? blockIdx.y * 4 + warp : 0, r_step = CTA_WORKERS ? gridDim.y * 4 : 1;
 #pragma unroll 1
-    for (int r = blockIdx.y * 4 + warp; r < n_rows; r += gridDim.y * 4) {
+    for (int r = r_first; r < n_rows; r += r_step) {
         float m = -INFINITY, l = 0.0f;
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         constexpr int AT_ONCE = 8;                   // parts whose loads are in flight together
@@ -668,11 +711,11 @@ template <int BITS, bool M16, int NT>
 int launch_rows(const ChunkParams &p, cudaStream_t st)
 {
     using S = Stage<BITS, M16>;
-    constexpr size_t steps = WARPS * (STAGES * S::BYTES + Queries<NT>::BYTES), smem = steps > MERGE_BYTES<NT> ? steps : MERGE_BYTES<NT>;
+    constexpr size_t smem = WARPS * (STAGES * S::BYTES + Queries<NT>::BYTES);
     static std::atomic<unsigned long long> allowed{0};
     const int rc = squat_allow_smem(reinterpret_cast<const void *>(chunk_rows_kernel<BITS, M16, NT>), smem, allowed);
     if (rc != SQUAT_OK) return rc;
-    return squat_launch(chunk_rows_kernel<BITS, M16, NT>, p.n_cta, THREADS, smem, st, p);
+    return squat_launch(chunk_rows_kernel<BITS, M16, NT>, p.n_workers / WARPS, THREADS, smem, st, p);
 }
 template <int NT>
 int launch_rows_tiles(const ChunkParams &p, int bits, int meta16, cudaStream_t st)
@@ -698,19 +741,20 @@ ChunkKernels kernels_for(long long n_q, long long n_seqs, long long max_q, int q
     if (k.tiles && n_q == n_seqs * max_q) k.eights = 0;      // sequences of one length, all of them in the other kernel
     return k;
 }
-int rows_ctas(int eights) { return squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : eights == 3 ? CTAS<3> : CTAS<4>); }
-int matrix_ctas(int tiles) { return squat_sm_count() * (tiles == 2 ? 1 : 2); }
-size_t part_floats(int n_cta, int rows) { return 2 * (size_t)n_cta * rows * (D + 2); }
-void use_part(ChunkParams &p, float *at, int n_cta, int rows)
+int rows_workers(int eights) { return WARPS * squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : eights == 3 ? CTAS<3> : CTAS<4>); }
+int matrix_workers(int tiles) { return squat_sm_count() * (tiles == 2 ? 1 : 2); }
+size_t part_floats(int workers, int rows) { return 2 * (size_t)workers * rows * (D + 2); }
+void use_part(ChunkParams &p, float *at, int workers, int rows)
 {
-    p.n_cta = n_cta;
+    p.n_workers = workers;
     p.part = at;
-    p.ml = at + 2 * (size_t)n_cta * rows * D;
+    p.ml = at + 2 * (size_t)workers * rows * D;
 }
 template <int ROWS>
 int launch_combine(const ChunkParams &p, cudaStream_t st)
 {
-    return squat_launch(chunk_combine_kernel<ROWS>, dim3((unsigned)p.n_cta, ROWS >= 16 ? ROWS / 16 : 1), D, 0, st, p);
+    if (ROWS >= 128) return squat_launch(chunk_combine_kernel<ROWS, 128, true>, dim3((unsigned)p.n_workers, ROWS / 16), D, 0, st, p);
+    return squat_launch(chunk_combine_kernel<ROWS, STEP, false>, dim3((unsigned)(p.n_workers / WARPS)), D, 0, st, p);
 }
 
 }  // namespace
@@ -719,7 +763,7 @@ size_t squat_chunk_workspace_floats(int n_q, int n_q_heads, int n_kv_heads, int 
 {
     (void)n_q;
     const ChunkKernels k = kernels_for(-1, 1, max_q, n_q_heads / n_kv_heads);
-    return part_floats(rows_ctas(k.eights), 8 * k.eights) + (k.tiles ? part_floats(matrix_ctas(k.tiles), 128 * k.tiles) : 0);
+    return part_floats(rows_workers(k.eights), 8 * k.eights) + (k.tiles ? part_floats(matrix_workers(k.tiles), 128 * k.tiles) : 0);
 }
 
 int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, float *workspace, int max_q, cudaStream_t st)
@@ -738,16 +782,16 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
         many.max_rows = 0x7fffffff;
         many.min_tiles = 4;
         many.start = 2;
-        use_part(many, workspace, matrix_ctas(k.tiles), 128 * k.tiles);
-        workspace += part_floats(many.n_cta, 128 * k.tiles);
+        use_part(many, workspace, matrix_workers(k.tiles), 128 * k.tiles);
+        workspace += part_floats(many.n_workers, 128 * k.tiles);
         rc = squat_launch_chunk_matrix(many, k.tiles, pool->bits, pool->meta16, st);
     }
     if (rc == SQUAT_OK && k.eights) {
         few.min_rows = 1;
         few.max_rows = k.tiles ? FEW_ROWS : 0x7fffffff;
-        few.min_tiles = 4;
-        few.start = 3;
-        use_part(few, workspace, rows_ctas(k.eights), 8 * k.eights);
+        few.min_tiles = 3;
+        few.start = 2;
+        use_part(few, workspace, rows_workers(k.eights), 8 * k.eights);
         switch (k.eights) {
             case 1: rc = launch_rows_tiles<1>(few, pool->bits, pool->meta16, st); break;
             case 2: rc = launch_rows_tiles<2>(few, pool->bits, pool->meta16, st); break;

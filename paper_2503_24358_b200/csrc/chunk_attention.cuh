@@ -1,17 +1,15 @@
-// Attention of new tokens over a paged cache: parameters, and how the work is dealt to CTAs (chunk_attention.cu).
+// Attention of new tokens over a paged cache: parameters, and how the work is dealt out (chunk_attention.cu, chunk_attention_mma.cu).
 //
 // An item is (sequence, KV head, R rows), a row being a query of one of the KV head's query heads: row r of a sequence is query
-// r / qpk of head h qpk + r mod qpk.  Its work is tiles of 128 tokens: the sequence's cached tokens, then as many of its
-// rows in full precision as the item's last query sees.  What an item costs besides (its queries, its first loads, its result) counts
-// as `start` tiles in front of them.  All items stand in one line, and CTA c takes places [c per, (c + 1) per) of it, whatever
-// sequences they belong to: a long sequence among short ones, or a single one, is spread over the GPU without the host knowing
-// a length.  An item that begins and ends within a CTA is finished there; of one that crosses a border, every CTA leaves (sum,
-// maximum, denominator) in the workspace and chunk_combine_kernel adds them up.  A CTA has at most two such parts: of the item
-// that it begins in the middle of (slot 2 c), and of the one that it begins and does not finish (slot 2 c + 1).
+// r / qpk of head h qpk + r mod qpk.  Its work is tiles of U tokens: the sequence's cached tokens, then as many of its rows in
+// full precision as the item's last query sees.  What an item costs besides (its queries, its first loads, its result) counts
+// as `start` tiles in front of them.  All items stand in one line, and worker w (a CTA, or a warp) takes places [w per, (w + 1) per)
+// of it, whatever sequences they belong to: a long sequence among short ones, or a single one, is spread over the GPU without the
+// host knowing a length.  An item that begins and ends within a worker's places is finished there; of one that crosses a border,
+// every worker leaves (sum, maximum, denominator) in the workspace and chunk_combine_kernel adds them up.  A worker has at most two
+// such parts: of the item that it begins in the middle of (slot 2 w), and of the one that it begins and does not finish (slot 2 w + 1).
 #pragma once
 #include "pages.cuh"
-
-constexpr int CHUNK_TILE = 128;                      // tokens
 
 struct ChunkParams {
     const __nv_bfloat16 *q;
@@ -26,8 +24,8 @@ struct ChunkParams {
     long long knt, knh, vnt, vnh;
     float scale_log2;                                // softmax scale / ln 2
     int min_rows, max_rows;                          // the kernel's sequences: those with so many rows
-    int n_cta, min_tiles, start;                     // CTAs that share the work, the least that one takes, and what an item costs besides its tiles
-    float *part, *ml;                                // [2 n_cta][R][D], [2 n_cta][R][2]
+    int n_workers, min_tiles, start;                 // who share the work, the least that one takes, and what an item costs besides its tiles
+    float *part, *ml;                                // [2 n_workers][R][D], [2 n_workers][R][2]
     unsigned *status;
 };
 
@@ -59,19 +57,19 @@ __device__ __forceinline__ int chunk_sees(const ChunkParams &p, const ChunkSeq &
 template <int R>
 __device__ __forceinline__ int chunk_row_tiles(const ChunkParams &p, const ChunkSeq &s) { return (int)(((long long)s.nq * p.qpk + R - 1) / R); }
 // tiles of the sequence's rows qt R .. of one head; at least one, which writes the zeros of rows that see nothing
-template <int R>
+template <int R, int U>
 __device__ __forceinline__ int chunk_tiles(const ChunkParams &p, const ChunkSeq &s, int qt)
 {
     const int last = (int)(min((long long)s.nq * p.qpk, (long long)(qt + 1) * R) - 1) / p.qpk;
-    const int n = (s.cached + CHUNK_TILE - 1) / CHUNK_TILE + (chunk_sees(p, s, last) + CHUNK_TILE - 1) / CHUNK_TILE;
+    const int n = (s.cached + U - 1) / U + (chunk_sees(p, s, last) + U - 1) / U;
     return max(n, 1);
 }
-template <int R>
+template <int R, int U>
 __device__ __forceinline__ long long chunk_head_tiles(const ChunkParams &p, const ChunkSeq &s)
 {
     const int n = chunk_row_tiles<R>(p, s);
     long long sum = 0;
-    for (int qt = 0; qt < n; ++qt) sum += p.start + chunk_tiles<R>(p, s, qt);
+    for (int qt = 0; qt < n; ++qt) sum += p.start + chunk_tiles<R, U>(p, s, qt);
     return sum;
 }
 
@@ -81,27 +79,27 @@ struct ChunkPlace {
 };
 struct ChunkShared {
     long long sums[33];
-    ChunkPlace found;
+    ChunkPlace found[4];
 };
 
-// All threads of the CTA (a multiple of 32, at most 1024) call this.  per: places per CTA, total: of all sequences.
-template <int R>
+// All threads of the CTA (a multiple of 32, at most 1024) call this.  per: places per worker, total: of all sequences.
+template <int R, int U>
 __device__ __forceinline__ void chunk_share(const ChunkParams &p, ChunkShared &sm, long long &per, long long &total)
 {
     long long mine = 0;
-    for (int i = threadIdx.x; i < p.n_seqs; i += blockDim.x) mine += chunk_head_tiles<R>(p, chunk_seq(p, i)) * p.H;
+    for (int i = threadIdx.x; i < p.n_seqs; i += blockDim.x) mine += chunk_head_tiles<R, U>(p, chunk_seq(p, i)) * p.H;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     if ((threadIdx.x & 31) == 0) sm.sums[threadIdx.x >> 5] = mine;
     __syncthreads();
     total = 0;
     for (int w = 0; w < (int)blockDim.x >> 5; ++w) total += sm.sums[w];
-    per = max((total + p.n_cta - 1) / p.n_cta, (long long)p.min_tiles);
+    per = max((total + p.n_workers - 1) / p.n_workers, (long long)p.min_tiles);
     __syncthreads();
 }
-// The item that holds place `at` of the line (at < total), for all threads.
-template <int R>
-__device__ __forceinline__ ChunkPlace chunk_locate(const ChunkParams &p, ChunkShared &sm, long long at)
+// The items that hold places first, first + per, .. of the line, N of them (those behind its end stay unknown), in sm.found.
+template <int R, int U, int N>
+__device__ __forceinline__ void chunk_locate(const ChunkParams &p, ChunkShared &sm, long long first, long long per)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     long long before = 0;
@@ -111,7 +109,7 @@ __device__ __forceinline__ ChunkPlace chunk_locate(const ChunkParams &p, ChunkSh
         long long head = 0, sum;
         if (i < p.n_seqs) {
             s = chunk_seq(p, i);
-            head = chunk_head_tiles<R>(p, s);
+            head = chunk_head_tiles<R, U>(p, s);
         }
         sum = head * p.H;
 #pragma unroll
@@ -124,17 +122,20 @@ __device__ __forceinline__ ChunkPlace chunk_locate(const ChunkParams &p, ChunkSh
         long long end = before + sum;
         for (int w = 0; w < warp; ++w) end += sm.sums[w];
         const long long begin = end - head * p.H;
-        if (head > 0 && at >= begin && at < end) {
-            long long rest = (at - begin) % head;
-            int qt = 0;
-            for (int n; rest >= (n = p.start + chunk_tiles<R>(p, s, qt)); ++qt) rest -= n;
-            sm.found = {i, (int)((at - begin) / head), qt, (int)rest};
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const long long at = first + k * per;
+            if (head > 0 && at >= begin && at < end) {
+                long long rest = (at - begin) % head;
+                int qt = 0;
+                for (int n; rest >= (n = p.start + chunk_tiles<R, U>(p, s, qt)); ++qt) rest -= n;
+                sm.found[k] = {i, (int)((at - begin) / head), qt, (int)rest};
+            }
         }
         for (int w = 0; w < warps; ++w) before += sm.sums[w];
         __syncthreads();
-        if (before > at) break;
+        if (before > first + (N - 1) * per) break;
     }
-    return sm.found;
 }
 // To the next item.
 template <int R>
@@ -174,16 +175,32 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
-// Code c of the low half of `word` and of the high half, as a pair of binary16 numbers.
+// Code c of the low half of `word` and of the high half under the exponent of 2^(10 - s), s the bit where it stands (after one shift
+// for the upper codes): a pair of binary16 numbers, bias + code.
 template <int BITS>
-__device__ __forceinline__ __half2 code_pair(uint32_t word, int c)
-{
-    constexpr int IN_PLACE = BITS == 2 ? 5 : 2;      // codes whose bits lie within a binary16's significand as they are
-    const int s = BITS * (c < IN_PLACE ? c : c - IN_PLACE);
-    const uint32_t src = c < IN_PLACE ? word : word >> (BITS * IN_PLACE);
-    const uint32_t bias = (uint32_t)(25 - s) << 10 | (uint32_t)(25 - s) << 26, mask = ((1u << BITS) - 1u) * 0x00010001u << s;
-    return __hsub2(as_half2((src & mask) | bias), as_half2(bias));
-}
+__device__ __forceinline__ constexpr int code_shift(int c) { return BITS * (c < (BITS == 2 ? 5 : 2) ? c : c - (BITS == 2 ? 5 : 2)); }
+template <int BITS>
+__device__ __forceinline__ constexpr uint32_t code_bias(int c) { return (uint32_t)(25 - code_shift<BITS>(c)) * 0x04000400u; }
+// The biases in registers, where the compiler has to keep them: mask (its immediate) and bias are then one logic instruction, not two.
+template <int BITS>
+struct CodeBias {
+    static constexpr int IN_PLACE = BITS == 2 ? 5 : 2;      // codes whose bits lie within a binary16's significand as they are
+    uint32_t at[IN_PLACE];
+    __device__ __forceinline__ CodeBias()
+    {
+#pragma unroll
+        for (int c = 0; c < IN_PLACE; ++c) asm volatile("mov.b32 %0, %1;" : "=r"(at[c]) : "r"(code_bias<BITS>(c)));
+    }
+    __device__ __forceinline__ uint32_t biased(uint32_t word, int c) const
+    {
+        const uint32_t src = c < IN_PLACE ? word : word >> (BITS * IN_PLACE), mask = ((1u << BITS) - 1u) * 0x00010001u << code_shift<BITS>(c);
+        uint32_t d;
+        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(src), "r"(mask), "r"(at[c % IN_PLACE]));
+        return d;
+    }
+    // the codes themselves
+    __device__ __forceinline__ __half2 codes(uint32_t word, int c) const { return __hsub2(as_half2(biased(word, c)), as_half2(code_bias<BITS>(c))); }
+};
 template <int BITS>
 __device__ __forceinline__ float code_float(uint32_t word, int pos) { return (float)(word >> (BITS * pos) & ((1u << BITS) - 1u)); }
 

@@ -17,7 +17,7 @@
 
 namespace {
 
-constexpr int D = SQUAT_D, T = CHUNK_TILE;
+constexpr int D = SQUAT_D, T = 128;                  // tokens of a tile
 constexpr float P_SHIFT = 8.0f, GROW = 6.0f;
 constexpr int OPERAND = T * D * 2;                   // bytes of a tile of 128 rows in shared memory: two halves of 64 channels
 
@@ -128,6 +128,7 @@ struct Producer {
     static constexpr int ROW = D * BITS / 8, NG = D / G;
     const ChunkParams &p;
     const ChunkSeq &sq;
+    const CodeBias<BITS> &bias;
     int h, most, ct, group32, sub, unit;             // the thread's 32 tokens of a tile, its first of them, its channels
 
     // first token of the thread's 32 in the pool for tile t; -1: past the cached tokens
@@ -156,7 +157,7 @@ struct Producer {
         }
     }
     // the pair of codes that becomes register m of a unit
-    __device__ __forceinline__ static __half2 pair(const Units<BITS> &u, int i, int m) { return BITS == 2 ? code_pair<BITS>(u.code[i][0], m) : code_pair<BITS>(u.code[i][m / 4 * (BITS / 2 - 1)], m % 4); }
+    __device__ __forceinline__ __half2 pair(const Units<BITS> &u, int i, int m) const { return BITS == 2 ? bias.codes(u.code[i][0], m) : bias.codes(u.code[i][m / 4 * (BITS / 2 - 1)], m % 4); }
     // channels (within the unit) of register m
     __device__ __forceinline__ static int lo_of_reg(int m) { return BITS == 2 ? m : m / 4 * 8 + m % 4; }
     __device__ __forceinline__ static int hi_of_reg(int m) { return lo_of_reg(m) + (BITS == 2 ? 8 : 4); }
@@ -179,11 +180,12 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
     ChunkParams p = params;
     grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
     long long per, total;
-    chunk_share<S::ROWS>(p, sh.place, per, total);
+    chunk_share<S::ROWS, T>(p, sh.place, per, total);
     long long at = per * blockIdx.x;
     if (at >= total) return;
     const long long end = min(at + per, total);
-    ChunkPlace pl = chunk_locate<S::ROWS>(p, sh.place, at);
+    chunk_locate<S::ROWS, T, 1>(p, sh.place, at, per);
+    ChunkPlace pl = sh.place.found[0];
     ChunkSeq sq = chunk_seq(p, pl.seq);
     if (warp == MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"((unsigned)S::TMEM) : "memory");
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
     unsigned kv = 0, turns = 0, segments = 0;        // tiles of tokens, scores of a row tile, and segments so far
 
     while (at < end) {
-        const int tiles = chunk_tiles<S::ROWS>(p, sq, pl.qt), begin = pl.at, stop = (int)min((long long)p.start + tiles, begin + (end - at));
+        const int tiles = chunk_tiles<S::ROWS, T>(p, sq, pl.qt), begin = pl.at, stop = (int)min((long long)p.start + tiles, begin + (end - at));
         const int ta = max(begin - p.start, 0), tb = max(stop - p.start, 0), n = tb - ta;
         const int rows = sq.nq * p.qpk, row0 = pl.qt * S::ROWS, n_rows = min(S::ROWS, rows - row0), last = row0 + n_rows - 1;
         const int ct = (sq.cached + T - 1) / T, most = chunk_sees(p, sq, last / p.qpk);
@@ -368,7 +370,8 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
             } else if (warp < MMA_WARP) {
                 // ------------------------------------------------------------ producers
                 const int pt = tid - S::SOFT;
-                const Pr pr{p, sq, pl.h, most, ct, pt / 32, pt / 8 % 4, pt % 8};
+                const CodeBias<BITS> bias;
+                const Pr pr{p, sq, bias, pl.h, most, ct, pt / 32, pt / 8 % 4, pt % 8};
                 const int row0_sm = 32 * pr.group32 + pr.sub;
                 __half2 ks_top = __float2half2_rn(0.0f), kz_top = ks_top, vs_top = ks_top, vz_top = ks_top;
                 float k_top = 0.0f, v_top = 0.0f;
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
                             for (int i = 0; i < 8; ++i) {
                                 uint32_t y[8];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(Pr::pair(ku, i, e), s2[e], z2[e]));
+                                for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(pr.pair(ku, i, e), s2[e], z2[e]));
                                 store_unit(k_to, row0_sm + 4 * i, pr.unit, y);
                             }
                         } else {
@@ -466,7 +469,7 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
                                     vs_top = __hmax2(vs_top, __habs2(s2));
                                     vz_top = __hmax2(vz_top, __habs2(z2));
 #pragma unroll
-                                    for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(Pr::pair(vu, i, e), s2, z2));
+                                    for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(pr.pair(vu, i, e), s2, z2));
                                 } else {
 #pragma unroll
                                     for (int e = 0; e < 8; ++e)
@@ -599,7 +602,7 @@ int launch_matrix(const ChunkParams &p, cudaStream_t st)
     static std::atomic<unsigned long long> allowed{0};
     const int rc = squat_allow_smem(reinterpret_cast<const void *>(chunk_matrix_kernel<BITS, G, M16, TILES>), S::SMEM, allowed);
     if (rc != SQUAT_OK) return rc;
-    return squat_launch(chunk_matrix_kernel<BITS, G, M16, TILES>, p.n_cta, S::THREADS, S::SMEM, st, p);
+    return squat_launch(chunk_matrix_kernel<BITS, G, M16, TILES>, p.n_workers, S::THREADS, S::SMEM, st, p);
 }
 template <int TILES>
 int launch_matrix_tiles(const ChunkParams &p, int bits, int meta16, cudaStream_t st)

@@ -18,6 +18,10 @@ static struct {
     __typeof__(&squat_dequantize) deq;
     __typeof__(&squat_dequantize_m16) deq_m16;
     __typeof__(&squat_decode_attention_ex) attend;
+    __typeof__(&squat_rope_apply) rope;
+    __typeof__(&squat_pages_write) pages_write;
+    __typeof__(&squat_pages_read) pages_read;
+    __typeof__(&squat_chunk_attention) chunk;
 } lib;
 
 /* n integers (None: 0) out of args */
@@ -46,9 +50,9 @@ static int integers(PyObject *const *args, Py_ssize_t given, Py_ssize_t n, ll *a
 
 static PyObject *bind(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
-    ll a[7];
+    ll a[11];
     (void)self;
-    if (!integers(args, n, 7, a)) return NULL;
+    if (!integers(args, n, 11, a)) return NULL;
     lib.keys = (__typeof__(lib.keys))P(0);
     lib.keys_m16 = (__typeof__(lib.keys_m16))P(1);
     lib.values = (__typeof__(lib.values))P(2);
@@ -56,6 +60,10 @@ static PyObject *bind(PyObject *self, PyObject *const *args, Py_ssize_t n)
     lib.deq = (__typeof__(lib.deq))P(4);
     lib.deq_m16 = (__typeof__(lib.deq_m16))P(5);
     lib.attend = (__typeof__(lib.attend))P(6);
+    lib.rope = (__typeof__(lib.rope))P(7);
+    lib.pages_write = (__typeof__(lib.pages_write))P(8);
+    lib.pages_read = (__typeof__(lib.pages_read))P(9);
+    lib.chunk = (__typeof__(lib.chunk))P(10);
     Py_RETURN_NONE;
 }
 
@@ -121,11 +129,74 @@ static PyObject *decode_attention(PyObject *self, PyObject *const *args, Py_ssiz
     return PyLong_FromLong(rc);
 }
 
+/* the arguments of squat_rope_apply */
+static PyObject *rope_apply(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    ll a[23];
+    int rc;
+    (void)self;
+    if (!integers(args, n, 23, a)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.rope(P(0), P(1), I(2), a[3], I(4), I(5), I(6), I(7), P(8), I(9), a[10], a[11], P(12), a[13], a[14], P(15), I(16), a[17], a[18], P(19), a[20], a[21], P(22));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* the arguments of squat_pages_write */
+static PyObject *pages_write(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    ll a[14];
+    int rc;
+    (void)self;
+    if (!integers(args, n, 14, a)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.pages_write(P(0), P(1), P(2), I(3), I(4), P(5), a[6], a[7], P(8), a[9], a[10], P(11), (size_t)a[12], P(13));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* the arguments of squat_pages_read */
+static PyObject *pages_read(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    ll a[11];
+    int rc;
+    (void)self;
+    if (!integers(args, n, 11, a)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.pages_read(P(0), P(1), I(2), I(3), P(4), a[5], a[6], P(7), a[8], a[9], P(10));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* softmax_scale, then the other arguments of squat_chunk_attention in their order */
+static PyObject *chunk_attention(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    ll a[29];
+    int rc;
+    (void)self;
+    if (n < 1) {
+        PyErr_SetString(PyExc_TypeError, "30 arguments expected");
+        return NULL;
+    }
+    const double scale = PyFloat_AsDouble(args[0]);
+    if (scale == -1.0 && PyErr_Occurred()) return NULL;
+    if (!integers(args + 1, n - 1, 29, a)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    rc = lib.chunk(P(0), I(1), I(2), a[3], a[4], P(5), I(6), P(7), P(8), P(9), I(10), P(11), P(12), I(13), a[14], a[15], a[16], a[17], P(18), P(19), I(20), I(21), (float)scale,
+                   P(22), a[23], a[24], P(25), P(26), (size_t)a[27], P(28));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of the library's functions"},
     {"quantize_keys", (PyCFunction)(void (*)(void))quantize_keys, METH_FASTCALL, NULL},
     {"quantize_values", (PyCFunction)(void (*)(void))quantize_values, METH_FASTCALL, NULL},
     {"dequantize", (PyCFunction)(void (*)(void))dequantize, METH_FASTCALL, NULL},
+    {"rope_apply", (PyCFunction)(void (*)(void))rope_apply, METH_FASTCALL, NULL},
+    {"pages_write", (PyCFunction)(void (*)(void))pages_write, METH_FASTCALL, NULL},
+    {"pages_read", (PyCFunction)(void (*)(void))pages_read, METH_FASTCALL, NULL},
+    {"chunk_attention", (PyCFunction)(void (*)(void))chunk_attention, METH_FASTCALL, NULL},
     {"decode_attention", (PyCFunction)(void (*)(void))decode_attention, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_squatcall", "direct calls into libsquat", -1, methods, NULL, NULL, NULL, NULL};
