@@ -16,7 +16,9 @@
 //   - Values, transposed: channels are the 16 side.  Lane (g, q) holds tokens 16 k + 2 q, + 1, + 8, + 9, channels 16 g .. 16 g + 15.
 //     The halves of two tokens' words are joined first, so a pair is one channel of two tokens, which is the order of this operand.
 //     Its sums stand at the lane that holds the rows' maxima.
-//   - A step's codes and metadata come through shared memory by cp.async, two steps ahead.
+//   - A step's codes and metadata come through shared memory by cp.async, a step ahead.
+// The loops are rolled where the registers allow it: straight-line code of a step, met once by a short sequence, takes longer to be
+// fetched than to be executed.
 // Binary16 keeps 11 significant bits, three more than bf16: the result's own rounding to bf16 is what is left.  Magnitudes
 // beyond its range (or values that all lie below 2^-8, where it would lose them) are noticed on the way, and the
 // segment is done again with bf16 operands.  Weights carry a factor of 2^8, so that those down to 2^-32 of the largest are not lost.
@@ -25,7 +27,7 @@
 namespace {
 
 constexpr int D = SQUAT_D;
-constexpr int THREADS = 128, WARPS = 4, STEP = 32, STAGES = 3;     // tokens per warp and step, steps in shared memory
+constexpr int THREADS = 128, WARPS = 4, STEP = 32, STAGES = 2;     // tokens per warp and step, steps in shared memory
 constexpr float P_SHIFT = 8.0f;
 
 template <int BITS, bool M16>
@@ -35,8 +37,9 @@ struct Stage {                                       // one step's part of the c
     static constexpr int KC = 0, VC = STEP * ROW, KS = 2 * STEP * ROW, KZ = KS + 4 * QUARTER, VS = KZ + 4 * QUARTER, VZ = VS + STEP * 4 * MS;
     static constexpr int BYTES = VZ + STEP * 4 * MS;
 };
+// CTAs to an SM
 template <int NT>
-constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;  // to an SM
+constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;
 
 __device__ __forceinline__ void cp16(unsigned dst, const void *src)
 {
@@ -72,33 +75,20 @@ struct Range {
     int odd_first, odd_last;                         // range of rows in full precision with infinities or NaN among their values
 };
 
-// The other operand of the scores: rows 8 t + g, pairs 2 kk and 2 kk + 1 of the lane's channels.  In registers; with four times eight rows,
-// whose sums take half of them, in the warp's own shared memory.
+// The other operand of the scores: rows 8 t + g, the lane's 16 pairs of channels, in the warp's own shared memory.
 template <int NT>
 struct Queries {
-    static constexpr bool IN_SMEM = NT == 4;
-    static constexpr int BYTES = IN_SMEM ? NT * 16 * 32 * 4 : 0;
-    uint32_t reg[IN_SMEM ? 1 : NT * 16];
-    uint32_t *smem;                                  // the lane's place: [t][kk / 2][lane][4]
-    __device__ __forceinline__ void put(int t, const uint32_t (&x)[16])
+    static constexpr int BYTES = NT * 16 * 32 * 4;
+    uint32_t *smem;                                  // the lane's place: [t][pair / 4][lane][4]
+    __device__ __forceinline__ void put(int t, const uint32_t (&x)[16]) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (IN_SMEM) *reinterpret_cast<uint4 *>(smem + (t * 4 + i) * 128) = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-            else
-#pragma unroll
-                for (int e = 0; e < 4; ++e) reg[IN_SMEM ? 0 : t * 16 + 4 * i + e] = x[4 * i + e];
-        }
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(smem + (t * 4 + i) * 128) = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
     }
-    __device__ __forceinline__ void get(int t, int kk, uint32_t (&b)[2]) const
+    __device__ __forceinline__ void get(int t, int four, uint32_t (&b)[4]) const       // pairs 4 four .. + 3
     {
-        if (IN_SMEM) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(smem + (t * 4 + kk / 2) * 128 + kk % 2 * 2);
-            b[0] = v.x; b[1] = v.y;
-        } else {
-            b[0] = reg[IN_SMEM ? 0 : t * 16 + 2 * kk];
-            b[1] = reg[IN_SMEM ? 0 : t * 16 + 2 * kk + 1];
-        }
+        const uint4 v = *reinterpret_cast<const uint4 *>(smem + (t * 4 + four) * 128);
+        b[0] = v.x; b[1] = v.y; b[2] = v.z; b[3] = v.w;
     }
 };
 
@@ -147,12 +137,11 @@ __device__ __forceinline__ void softmax_step(Acc<NT> &acc, float (&s)[NT][2][4],
     }
 }
 
-// Scales or zero-points of pairs 2 kk and 2 kk + 1 of the lane's 32 channels: channels (lo, lo + HALF) and (lo + 1, lo + 1 + HALF).
+// Scales or zero-points of two neighbouring pairs: channels (lo, lo + HALF) and (lo + 1, lo + 1 + HALF) of the lane's 32.
 template <int BITS, bool M16>
-__device__ __forceinline__ void meta_pairs(const unsigned char *from, int kk, __half2 (&y)[2])
+__device__ __forceinline__ void meta_pairs(const unsigned char *from, int lo, __half2 (&y)[2])
 {
     constexpr int HALF = BITS == 2 ? 8 : 4;          // codes in half a word; a pair is (c, c + HALF) of a word
-    const int lo = 2 * kk / HALF * 2 * HALF + 2 * kk % HALF;
     if (M16) {
         const uint32_t a = reinterpret_cast<const uint32_t *>(from)[lo / 2], b = reinterpret_cast<const uint32_t *>(from)[(lo + HALF) / 2];
         y[0] = as_half2(pair16(a, b, 0));
@@ -192,61 +181,62 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, const CodeB
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) alike[t][e] = 0.0f;
-        const unsigned char *ks = st + S::KS + q * S::QUARTER, *kz = st + S::KZ + q * S::QUARTER;
-        uint32_t w[4][BITS];                         // the lane's tokens g, g + 8, g + 16, g + 24
+        const unsigned char *ks = st + S::KS + q * S::QUARTER, *kz = st + S::KZ + q * S::QUARTER, *kc = st + S::KC + g * S::ROW + q * (S::ROW / 4);
+#pragma unroll 1
+        for (int wd = 0; wd < BITS; ++wd) {          // a word of codes: HALF pairs
+            uint32_t w[4];                           // of tokens g, g + 8, g + 16, g + 24
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned char *from = st + S::KC + (8 * e + g) * S::ROW + q * (S::ROW / 4);
-            if (BITS == 2) {
-                const uint2 v = *reinterpret_cast<const uint2 *>(from);
-                w[e][0] = v.x; w[e][1] = v.y;
-            } else {
-                const uint4 v = *reinterpret_cast<const uint4 *>(from);
-                w[e][0] = v.x; w[e][1] = v.y; w[e][BITS - 2] = v.z; w[e][BITS - 1] = v.w;
-            }
-        }
+            for (int e = 0; e < 4; ++e) w[e] = *reinterpret_cast<const uint32_t *>(kc + 8 * e * S::ROW + 4 * wd);
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-            __half2 s2[2], z2[2];
-            if (!BF) {
-                meta_pairs<BITS, M16>(ks, kk, s2);
-                meta_pairs<BITS, M16>(kz, kk, z2);
-            }
-            uint32_t b[NT][2];
+            for (int four = 0; four < HALF / 4; ++four) {
+                uint32_t b4[NT][4];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) queries.get(t, kk, b[t]);
-            if (FOLD) {
-                // sum q (z + s c) = sum q z - sum (q s) B + sum (q s) (B + c): the first two are the same for every token, so they are
-                // products with rows that are all alike, made once for both halves
-                const uint32_t za[4] = {as_u32(z2[0]), as_u32(z2[0]), as_u32(z2[1]), as_u32(z2[1])};
-                const uint32_t b0 = code_bias<BITS>(2 * kk % HALF) | 0x80008000u, b1 = code_bias<BITS>((2 * kk + 1) % HALF) | 0x80008000u, ba[4] = {b0, b0, b1, b1};
+                for (int t = 0; t < NT; ++t) queries.get(t, wd * (HALF / 4) + four, b4[t]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    mma16<false>(alike[t], za, b[t][0], b[t][1]);
-                    b[t][0] = as_u32(__hmul2(as_half2(b[t][0]), s2[0]));
-                    b[t][1] = as_u32(__hmul2(as_half2(b[t][1]), s2[1]));
-                    mma16<false>(alike[t], ba, b[t][0], b[t][1]);
-                }
-            }
+                for (int two = 0; two < 2; ++two) {  // a product contracts two pairs of every lane of a quad
+                    const int c = 4 * four + 2 * two, lo = wd * 2 * HALF + c;
+                    __half2 s2[2], z2[2];
+                    if (!BF) {
+                        meta_pairs<BITS, M16>(ks, lo, s2);
+                        meta_pairs<BITS, M16>(kz, lo, z2);
+                    }
+                    uint32_t b[NT][2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                uint32_t a[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {        // token g or g + 8 of the half, pair 2 kk or 2 kk + 1
-                    const int m = 2 * kk + (e >> 1);
-                    const uint32_t word = w[2 * k + (e & 1)][m / HALF];
+                    for (int t = 0; t < NT; ++t) { b[t][0] = b4[t][2 * two]; b[t][1] = b4[t][2 * two + 1]; }
                     if (FOLD) {
-                        a[e] = bias.biased(word, m % HALF);
-                    } else if (!BF) {
-                        a[e] = as_u32(__hfma2(bias.codes(word, m % HALF), s2[e >> 1], z2[e >> 1]));
-                    } else {
-                        const int lo = m / HALF * 2 * HALF + m % HALF, hi = lo + HALF;
-                        a[e] = pack16<true>(fmaf(code_float<BITS>(word, m % HALF), meta_at<M16>(ks, lo), meta_at<M16>(kz, lo)),
-                                            fmaf(code_float<BITS>(word, m % HALF + HALF), meta_at<M16>(ks, hi), meta_at<M16>(kz, hi)));
+                        // sum q (z + s c) = sum q z - sum (q s) B + sum (q s) (B + c): the first two are the same for every token, so they
+                        // are products with rows that are all alike, made once for both halves
+                        const uint32_t za[4] = {as_u32(z2[0]), as_u32(z2[0]), as_u32(z2[1]), as_u32(z2[1])};
+                        const uint32_t b0 = code_bias<BITS>(c) | 0x80008000u, b1 = code_bias<BITS>(c + 1) | 0x80008000u, ba[4] = {b0, b0, b1, b1};
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            mma16<false>(alike[t], za, b[t][0], b[t][1]);
+                            b[t][0] = as_u32(__hmul2(as_half2(b[t][0]), s2[0]));
+                            b[t][1] = as_u32(__hmul2(as_half2(b[t][1]), s2[1]));
+                            mma16<false>(alike[t], ba, b[t][0], b[t][1]);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t a[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {        // token g or g + 8 of the half, the first or the second pair
+                            const uint32_t word = w[2 * k + (e & 1)];
+                            const int ce = c + (e >> 1);
+                            if (FOLD) {
+                                a[e] = bias.biased(word, ce);
+                            } else if (!BF) {
+                                a[e] = as_u32(__hfma2(bias.codes(word, ce), s2[e >> 1], z2[e >> 1]));
+                            } else {
+                                const int l = lo + (e >> 1), h = l + HALF;
+                                a[e] = pack16<true>(fmaf(code_float<BITS>(word, ce), meta_at<M16>(ks, l), meta_at<M16>(kz, l)),
+                                                    fmaf(code_float<BITS>(word, ce + HALF), meta_at<M16>(ks, h), meta_at<M16>(kz, h)));
+                            }
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) mma16<BF>(s[t][k], a, b[t][0], b[t][1]);
                     }
                 }
-#pragma unroll
-                for (int t = 0; t < NT; ++t) mma16<BF>(s[t][k], a, b[t][0], b[t][1]);
             }
         }
         if (FOLD)
@@ -266,8 +256,11 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, const CodeB
                 for (int e = 0; e < 4; ++e) range.score = max_nan(range.score, fabsf(s[t][k][e]));
     uint32_t pb[NT][2][2];
     softmax_step<NT, BF>(acc, s, scale_log2, pb);
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 2; ++k) {
+        uint32_t b[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) { b[t][0] = k ? pb[t][1][0] : pb[t][0][0]; b[t][1] = k ? pb[t][1][1] : pb[t][0][1]; }
         uint32_t w[4][BITS / 2];                     // 16 channels of the lane's four tokens
         float sc[4], zr[4];
 #pragma unroll
@@ -309,7 +302,7 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, const CodeB
                 }
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mma16<BF>(acc.o[t][i], a, pb[t][k][0], pb[t][k][1]);
+            for (int t = 0; t < NT; ++t) mma16<BF>(acc.o[t][i], a, b[t][0], b[t][1]);
         }
     }
 }
@@ -323,7 +316,7 @@ __device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &
     constexpr int HALF = BITS == 2 ? 8 : 4;
     const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     float s[NT][2][4];
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 2; ++k) {
         uint32_t x[2][16];
 #pragma unroll
@@ -335,44 +328,51 @@ __device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &
                 if (u < most) v = ldg128(p.k_new + (long long)(sq.k0 + u) * p.knt + (long long)h * p.knh + 32 * q + 8 * i);
                 x[e][4 * i] = v.x; x[e][4 * i + 1] = v.y; x[e][4 * i + 2] = v.z; x[e][4 * i + 3] = v.w;
             }
-            if (!BF)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {        // infinities and NaN are the same in either type
-                    const float lo = fabsf(bf16lo_to_f32(x[e][i])), hi = fabsf(bf16hi_to_f32(x[e][i]));
-                    range.k = fmaxf(range.k, fmaxf(lo < INFINITY ? lo : 0.0f, hi < INFINITY ? hi : 0.0f));
-                }
         }
+        float d[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][k][e] = 0.0f;
+            for (int e = 0; e < 4; ++e) d[t][e] = 0.0f;
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-            uint32_t a[4];
+        for (int four = 0; four < 4; ++four) {
+            uint32_t b[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) queries.get(t, four, b[t]);
+#pragma unroll
+            for (int two = 0; two < 2; ++two) {
+                uint32_t a[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int m = 4 * four + 2 * two + (e >> 1), lo = m / HALF * 2 * HALF + m % HALF;
+                    a[e] = pair16(x[e & 1][lo / 2], x[e & 1][(lo + HALF) / 2], lo);
+                    if (!BF) {                        // infinities and NaN are the same in either type
+                        const float v0 = fabsf(bf16lo_to_f32(a[e])), v1 = fabsf(bf16hi_to_f32(a[e]));
+                        range.k = fmaxf(range.k, fmaxf(v0 < INFINITY ? v0 : 0.0f, v1 < INFINITY ? v1 : 0.0f));
+                        a[e] = bf16_pair_to_f16(a[e]);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16<BF>(d[t], a, b[t][2 * two], b[t][2 * two + 1]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int m = 2 * kk + (e >> 1), lo = m / HALF * 2 * HALF + m % HALF;
-                a[e] = pair16(x[e & 1][lo / 2], x[e & 1][(lo + HALF) / 2], lo);
-                if (!BF) a[e] = bf16_pair_to_f16(a[e]);
+                const float v = u0 + 16 * k + g + 8 * (e >> 1) < sees[t][e & 1] ? d[t][e] : -INFINITY;
+                if (k == 0) s[t][0][e] = v;
+                else s[t][1][e] = v;
             }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                uint32_t b[2];
-                queries.get(t, kk, b);
-                mma16<BF>(s[t][k], a, b[0], b[1]);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (u0 + 16 * k + g + 8 * (e >> 1) >= sees[t][e & 1]) s[t][k][e] = -INFINITY;
     }
     uint32_t pb[NT][2][2];
     softmax_step<NT, BF>(acc, s, p.scale_log2, pb);
     bool odd = false;                                // an infinity or NaN among the lane's values
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 2; ++k) {
+        uint32_t b[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) { b[t][0] = k ? pb[t][1][0] : pb[t][0][0]; b[t][1] = k ? pb[t][1][1] : pb[t][0][1]; }
         uint32_t w[4][8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -403,7 +403,7 @@ __device__ __forceinline__ void full_step(const ChunkParams &p, const ChunkSeq &
                 if (!BF) a[e] = bf16_pair_to_f16(a[e]);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mma16<BF>(acc.o[t][i], a, pb[t][k][0], pb[t][k][1]);
+            for (int t = 0; t < NT; ++t) mma16<BF>(acc.o[t][i], a, b[t][0], b[t][1]);
         }
     }
     if (__any_sync(0xffffffffu, odd)) {
@@ -529,10 +529,10 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
     for (int i = 0; i < steps; ++i) {
         cp_wait<STAGES - 2>();
         __syncwarp();
+        if ((i + STAGES - 1) % 32 == 0) look_up(i + STAGES - 1);
+        load(i + STAGES - 1);                        // into the stage of the step before this one
         cached_step<BITS, M16, NT, BF>(stages + i % STAGES * S::BYTES, bias, g_shift, queries, p.scale_log2, acc, range);
         __syncwarp();
-        if ((i + STAGES - 1) % 32 == 0) look_up(i + STAGES - 1);
-        load(i + STAGES - 1);
     }
     cp_wait<0>();
     __syncwarp();
@@ -669,7 +669,7 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
     const ChunkSeq sq = chunk_seq(p, pl.seq);
     const long long parts = (first + chunk_tiles<ROWS, U>(p, sq, pl.qt) - 1) / per - c + 1;
     const int row0 = pl.qt * ROWS, n_rows = min(ROWS, sq.nq * p.qpk - row0);
-    const int r_first = CTA_WORKERS ? blockIdx.y * 4 + warp : 0, r_step = CTA_WORKERS ? gridDim.y * 4 : 1;
+    const int r_first = CTA_WORKERS ? blockIdx.y * 4 + warp : blockIdx.y, r_step = gridDim.y * (CTA_WORKERS ? 4 : 1);
 #pragma unroll 1
     for (int r = r_first; r < n_rows; r += r_step) {
         float m = -INFINITY, l = 0.0f;
@@ -744,9 +744,12 @@ ChunkKernels kernels_for(long long n_q, long long n_seqs, long long max_q, int q
 int rows_workers(int eights) { return WARPS * squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : eights == 3 ? CTAS<3> : CTAS<4>); }
 int matrix_workers(int tiles) { return squat_sm_count() * (tiles == 2 ? 1 : 2); }
 size_t part_floats(int workers, int rows) { return 2 * (size_t)workers * rows * (D + 2); }
-void use_part(ChunkParams &p, float *at, int workers, int rows)
+// Workers, at most as many as the longest sequences that the page table can hold would give work to, and their parts.
+void use_part(ChunkParams &p, float *at, int workers, int rows, int tile, int together)
 {
-    p.n_workers = workers;
+    const double tokens = (double)p.table_stride * p.pool.page_tokens + p.n_new, row_tiles = (double)p.n_q * p.qpk / rows + p.n_seqs;
+    const double most = row_tiles * p.H * (p.start + tokens / tile + 2.0) / p.min_tiles + 1.0;
+    p.n_workers = most < workers ? ((int)most + together - 1) / together * together : workers;
     p.part = at;
     p.ml = at + 2 * (size_t)workers * rows * D;
 }
@@ -754,7 +757,7 @@ template <int ROWS>
 int launch_combine(const ChunkParams &p, cudaStream_t st)
 {
     if (ROWS >= 128) return squat_launch(chunk_combine_kernel<ROWS, 128, true>, dim3((unsigned)p.n_workers, ROWS / 16), D, 0, st, p);
-    return squat_launch(chunk_combine_kernel<ROWS, STEP, false>, dim3((unsigned)(p.n_workers / WARPS)), D, 0, st, p);
+    return squat_launch(chunk_combine_kernel<ROWS, STEP, false>, dim3((unsigned)(p.n_workers / WARPS), ROWS / 4), D, 0, st, p);
 }
 
 }  // namespace
@@ -782,8 +785,8 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
         many.max_rows = 0x7fffffff;
         many.min_tiles = 4;
         many.start = 2;
-        use_part(many, workspace, matrix_workers(k.tiles), 128 * k.tiles);
-        workspace += part_floats(many.n_workers, 128 * k.tiles);
+        use_part(many, workspace, matrix_workers(k.tiles), 128 * k.tiles, 128, 1);
+        workspace += part_floats(matrix_workers(k.tiles), 128 * k.tiles);
         rc = squat_launch_chunk_matrix(many, k.tiles, pool->bits, pool->meta16, st);
     }
     if (rc == SQUAT_OK && k.eights) {
@@ -791,7 +794,7 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
         few.max_rows = k.tiles ? FEW_ROWS : 0x7fffffff;
         few.min_tiles = 3;
         few.start = 2;
-        use_part(few, workspace, rows_workers(k.eights), 8 * k.eights);
+        use_part(few, workspace, rows_workers(k.eights), 8 * k.eights, STEP, WARPS);
         switch (k.eights) {
             case 1: rc = launch_rows_tiles<1>(few, pool->bits, pool->meta16, st); break;
             case 2: rc = launch_rows_tiles<2>(few, pool->bits, pool->meta16, st); break;

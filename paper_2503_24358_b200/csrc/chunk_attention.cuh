@@ -41,7 +41,7 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams &p, int i)
     s.nq = max(min(b, p.n_q) - s.q0, 0);
     const long long room = p.pool.n_pages > 0 ? (long long)p.table_stride * p.pool.page_tokens : 0;
     s.cached = (int)min((long long)max(c, 0), room);
-    s.cached -= s.cached % p.G;
+    s.cached &= -p.G;                                // (a power of two)
     s.k0 = min(max(k0, 0), p.n_new);
     s.nk = min(max(nk, 0), p.n_new - s.k0);
     if (s.q0 != a || s.q0 + s.nq != b || s.cached != c || s.k0 != k0 || s.nk != nk) atomicOr(p.status, SQUAT_FLAG_PAGES);
@@ -126,10 +126,13 @@ __device__ __forceinline__ void chunk_locate(const ChunkParams &p, ChunkShared &
         for (int k = 0; k < N; ++k) {
             const long long at = first + k * per;
             if (head > 0 && at >= begin && at < end) {
-                long long rest = (at - begin) % head;
+                // (a sequence's places mostly fit 32 bits, whose division is a tenth of the other)
+                const unsigned long long off = at - begin;
+                const int in_head = (off | (unsigned long long)head) >> 32 ? (int)(off / head) : (int)((unsigned)off / (unsigned)head);
+                long long rest = (long long)off - in_head * head;
                 int qt = 0;
                 for (int n; rest >= (n = p.start + chunk_tiles<R, U>(p, s, qt)); ++qt) rest -= n;
-                sm.found[k] = {i, (int)((at - begin) / head), qt, (int)rest};
+                sm.found[k] = {i, in_head, qt, (int)rest};
             }
         }
         for (int w = 0; w < warps; ++w) before += sm.sums[w];
