@@ -23,9 +23,12 @@ constexpr int OPERAND = T * D * 2;                   // bytes of a tile of 128 r
 
 template <int TILES>
 struct Plan {
-    static constexpr int ROWS = 128 * TILES, STAGES = TILES, SOFT = 128 * TILES, THREADS = SOFT + 128 + 32;
+    static constexpr int ROWS = 128 * TILES, STAGES = TILES, SOFT = 128 * TILES, THREADS = SOFT + 256;
     static constexpr int CTAS = TILES == 2 ? 1 : 2;  // to an SM
     static constexpr int TMEM = 256 * TILES;         // columns: scores (and weights) of each tile, then sums of each tile
+    // registers of a thread at launch, and of the roles' threads after it
+    static constexpr int LAUNCH_REGS = TILES == 2 ? 128 : 80, SOFT_REGS = TILES == 2 ? 144 : 96, PRODUCER_REGS = TILES == 2 ? 160 : 112, PRODUCT_REGS = TILES == 2 ? 64 : 32;
+    static_assert(TILES * SOFT_REGS + PRODUCER_REGS + PRODUCT_REGS == (TILES + 2) * LAUNCH_REGS, "more registers than the block is launched with");
     static constexpr size_t SMEM = 1024 + (size_t)(TILES + 2 * STAGES) * OPERAND;
 };
 
@@ -117,61 +120,591 @@ __device__ __forceinline__ void unit_of_bf16(const uint32_t (&x)[8], bool bf, ui
     }
 }
 
-// Eight units of a thread (tokens 32 (thread / 32) + thread / 8 mod 4 + 4 i, unit thread mod 8): codes as loaded and what they need.
-template <int BITS>
-struct Units {
-    uint32_t code[8][BITS / 2];
-};
-
-template <int BITS, int G, bool M16, int TILES>
+// A producer's part of a tile of cached tokens: tokens 32 (thread / 32) + thread / 8 mod 4 + 4 i (one page, one group of keys), channels
+// 16 (thread mod 8) .. + 15.  Keys and values are asked for a tile ahead: the keys of the next tile while this one's values are made, and
+// the other way round.
+template <int BITS, int G, bool M16>
 struct Producer {
     static constexpr int ROW = D * BITS / 8, NG = D / G;
-    const ChunkParams &p;
-    const ChunkSeq &sq;
-    const CodeBias<BITS> &bias;
-    int h, most, ct, group32, sub, unit;             // the thread's 32 tokens of a tile, its first of them, its channels
+    const CodeBias<BITS> bias;
+    int sub, unit;                                   // thread / 8 mod 4, thread mod 8
+    uint32_t code[2][8][BITS / 2];                   // keys, values
+    uint4 ks[M16 ? 2 : 4], kz[M16 ? 2 : 4];          // the unit's scales and zero-points (keys)
+    float vs[8], vz[8];                              // the tokens' (values)
 
-    // first token of the thread's 32 in the pool for tile t; -1: past the cached tokens
-    __device__ __forceinline__ long long place(int seq, int t) const
-    {
-        const int at = t * T + 32 * group32;
-        if (t >= ct || at >= sq.cached) return -1;
-        const int pg = at / p.pool.page_tokens;
-        int page = __ldg(p.page_table + (long long)seq * p.table_stride + pg);
-        if ((unsigned)page >= (unsigned)p.pool.n_pages) {
-            atomicOr(p.status, SQUAT_FLAG_PAGES);
-            page = 0;
-        }
-        return (long long)page * p.pool.page_stride + (long long)h * p.pool.head_stride + (at - pg * p.pool.page_tokens);
-    }
-    __device__ __forceinline__ void load_codes(const unsigned char *codes, long long tok, Units<BITS> &u) const
+    __device__ __forceinline__ void load_codes(int side, const unsigned char *codes, long long tok)
     {
         const unsigned char *from = codes + (tok + sub) * ROW + unit * (2 * BITS);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (BITS == 2) u.code[i][0] = __ldg(reinterpret_cast<const uint32_t *>(from + 4 * i * ROW));
+            if (BITS == 2) code[side][i][0] = __ldg(reinterpret_cast<const uint32_t *>(from + 4 * i * ROW));
             else {
                 const uint2 v = __ldg(reinterpret_cast<const uint2 *>(from + 4 * i * ROW));
-                u.code[i][0] = v.x; u.code[i][BITS / 2 - 1] = v.y;
+                code[side][i][0] = v.x; code[side][i][BITS / 2 - 1] = v.y;
             }
         }
     }
-    // the pair of codes that becomes register m of a unit
-    __device__ __forceinline__ __half2 pair(const Units<BITS> &u, int i, int m) const { return BITS == 2 ? bias.codes(u.code[i][0], m) : bias.codes(u.code[i][m / 4 * (BITS / 2 - 1)], m % 4); }
-    // channels (within the unit) of register m
-    __device__ __forceinline__ static int lo_of_reg(int m) { return BITS == 2 ? m : m / 4 * 8 + m % 4; }
-    __device__ __forceinline__ static int hi_of_reg(int m) { return lo_of_reg(m) + (BITS == 2 ? 8 : 4); }
-    __device__ __forceinline__ static float code_at(const Units<BITS> &u, int i, int c)
+    __device__ __forceinline__ void load_keys(const PagePool &pool, long long tok)
     {
-        return BITS == 2 ? code_float<BITS>(u.code[i][0], c) : code_float<BITS>(u.code[i][c / 8 * (BITS / 2 - 1)], c % 8);
+        load_codes(0, pool.kc, tok);
+        const long long at = (tok / G * D + 16 * unit) * (M16 ? 2 : 4) / 16;
+#pragma unroll
+        for (int i = 0; i < (M16 ? 2 : 4); ++i) {
+            ks[i] = __ldg(static_cast<const uint4 *>(pool.ks) + at + i);
+            kz[i] = __ldg(static_cast<const uint4 *>(pool.kz) + at + i);
+        }
+    }
+    __device__ __forceinline__ void load_values(const PagePool &pool, long long tok)
+    {
+        load_codes(1, pool.vc, tok);
+        const long long at = (tok + sub) * NG + 16 * unit / G;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            vs[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(pool.vs) + at + 4 * i * NG)) : __ldg(static_cast<const float *>(pool.vs) + at + 4 * i * NG);
+            vz[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(pool.vz) + at + 4 * i * NG)) : __ldg(static_cast<const float *>(pool.vz) + at + 4 * i * NG);
+        }
+    }
+    // register m of a unit holds channels lo_of(m) and lo_of(m) + HALF
+    static constexpr int HALF = BITS == 2 ? 8 : 4;
+    __device__ __forceinline__ static constexpr int lo_of(int m) { return BITS == 2 ? m : m / 4 * 8 + m % 4; }
+    __device__ __forceinline__ __half2 pair(int side, int i, int m) const { return BITS == 2 ? bias.codes(code[side][i][0], m) : bias.codes(code[side][i][m / 4 * (BITS / 2 - 1)], m % 4); }
+    __device__ __forceinline__ float code_at(int side, int i, int c) const
+    {
+        return BITS == 2 ? code_float<BITS>(code[side][i][0], c) : code_float<BITS>(code[side][i][c / 8 * (BITS / 2 - 1)], c % 8);
+    }
+    __device__ __forceinline__ static float meta(const uint4 *x, int c)
+    {
+        const uint4 &v = x[c / (M16 ? 8 : 4)];
+        const int w = M16 ? c % 8 / 2 : c % 4;
+        const uint32_t u = w == 0 ? v.x : w == 1 ? v.y : w == 2 ? v.z : v.w;
+        return M16 ? __half2float(__ushort_as_half((unsigned short)(u >> (16 * (c & 1))))) : __uint_as_float(u);
+    }
+    __device__ __forceinline__ static uint32_t meta_word(const uint4 *x, int c)      // (binary16) channels c, c + 1
+    {
+        const uint4 &v = x[c / 8];
+        const int w = c % 8 / 2;
+        return w == 0 ? v.x : w == 1 ? v.y : w == 2 ? v.z : v.w;
+    }
+    __device__ __forceinline__ static __half2 meta_pair(const uint4 *x, int m)
+    {
+        const int lo = lo_of(m);
+        if (M16) return as_half2(pair16(meta_word(x, lo & ~1), meta_word(x, (lo + HALF) & ~1), lo));
+        return __floats2half2_rn(meta(x, lo), meta(x, lo + HALF));
+    }
+    template <bool BF>
+    __device__ __forceinline__ void store_keys(unsigned char *to, int row, __half2 &s_top, __half2 &z_top) const
+    {
+        if (!BF) {
+            __half2 s2[8], z2[8];
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                s2[m] = meta_pair(ks, m);
+                z2[m] = meta_pair(kz, m);
+                s_top = __hmax2(s_top, __habs2(s2[m]));
+                z_top = __hmax2(z_top, __habs2(z2[m]));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t y[8];
+#pragma unroll
+                for (int m = 0; m < 8; ++m) y[m] = as_u32(__hfma2(pair(0, i, m), s2[m], z2[m]));
+                store_unit(to, row + 4 * i, unit, y);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t y[8];
+#pragma unroll
+                for (int m = 0; m < 8; ++m) {
+                    const int lo = lo_of(m), hi = lo + HALF;
+                    y[m] = pack16<true>(fmaf(code_at(0, i, lo), meta(ks, lo), meta(kz, lo)), fmaf(code_at(0, i, hi), meta(ks, hi), meta(kz, hi)));
+                }
+                store_unit(to, row + 4 * i, unit, y);
+            }
+        }
+    }
+    template <bool BF>
+    __device__ __forceinline__ void store_values(unsigned char *to, int row, __half2 &s_top, __half2 &z_top) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t y[8];
+            if (!BF) {
+                const __half2 s2 = __float2half2_rn(vs[i]), z2 = __float2half2_rn(vz[i]);
+                s_top = __hmax2(s_top, __habs2(s2));
+                z_top = __hmax2(z_top, __habs2(z2));
+#pragma unroll
+                for (int m = 0; m < 8; ++m) y[m] = as_u32(__hfma2(pair(1, i, m), s2, z2));
+            } else {
+#pragma unroll
+                for (int m = 0; m < 8; ++m) y[m] = pack16<true>(fmaf(code_at(1, i, lo_of(m)), vs[i], vz[i]), fmaf(code_at(1, i, lo_of(m) + HALF), vs[i], vz[i]));
+            }
+            store_unit(to, row + 4 * i, unit, y);
+        }
     }
 };
+
+// A CTA's way along the line of items.
+struct Walk {
+    ChunkPlace pl;
+    ChunkSeq sq;
+    long long at, end;
+};
+struct Segment {                                     // tiles [ta, tb) of an item
+    int ta, tb, n, tiles, steps, row0, n_rows, last, ct, most;
+};
+template <int ROWS>
+__device__ __forceinline__ bool walk_segment(const ChunkParams &p, Walk &w, Segment &sg)
+{
+    while (w.at < w.end) {
+        sg.tiles = chunk_tiles<ROWS, T>(p, w.sq, w.pl.qt);
+        const int begin = w.pl.at, stop = (int)min((long long)p.start + sg.tiles, begin + (w.end - w.at));
+        sg.ta = max(begin - p.start, 0);
+        sg.tb = max(stop - p.start, 0);
+        sg.n = sg.tb - sg.ta;
+        sg.steps = stop - begin;
+        if (sg.n > 0) {
+            sg.row0 = w.pl.qt * ROWS;
+            sg.n_rows = min(ROWS, w.sq.nq * p.qpk - sg.row0);
+            sg.last = sg.row0 + sg.n_rows - 1;
+            sg.ct = (w.sq.cached + T - 1) / T;
+            sg.most = chunk_sees(p, w.sq, sg.last / p.qpk);
+            return true;
+        }
+        w.at += sg.steps;
+        if (w.at < w.end) chunk_next<ROWS>(p, w.pl, w.sq);
+    }
+    return false;
+}
+template <int ROWS>
+__device__ __forceinline__ void walk_on(const ChunkParams &p, Walk &w, const Segment &sg)
+{
+    w.at += sg.steps;
+    if (w.at < w.end) chunk_next<ROWS>(p, w.pl, w.sq);
+}
+// All roles: the segment begins (its queries may be stored), its queries are there, its sums have been taken; whether it is done again in bf16.
+template <int TILES>
+__device__ __forceinline__ void segment_begins(Shared<TILES> &sh)
+{
+    if (threadIdx.x == 0) {
+        sh.wide = 0;
+        sh.odd_first = 0x7fffffff;
+        sh.odd_last = -1;
+        sh.v_top = sh.k_top = 0;
+    }
+    __syncthreads();
+}
+template <int TILES>
+__device__ __forceinline__ bool too_wide(Shared<TILES> &sh, bool bf)
+{
+    const float k_top = __int_as_float(*(volatile int *)&sh.k_top), v_top = __int_as_float(*(volatile int *)&sh.v_top);
+    return !bf && (*(volatile int *)&sh.wide || !(k_top < 4096.0f) || !(v_top < 65000.0f) || (v_top < 0x1p-8f && v_top > 0.0f));
+}
+template <int TILES>
+__device__ __forceinline__ bool segment_again(Shared<TILES> &sh, bool bf)
+{
+    __syncthreads();
+    tc_fence_after();
+    const bool again = too_wide(sh, bf);
+    __syncthreads();
+    return again;
+}
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// 64 columns of a row's scores at a time; past the first `lim` of the tile they are -infinity.  (Loops of 64 columns, and the rare
+// cases apart: the roles' loops together have to stay within the instruction cache, or fetching them is what takes the time.)
+template <bool MASKED>
+__device__ __forceinline__ void load_scores(unsigned s_addr, int half, int lim, float (&x)[32], float (&y)[32])
+{
+    tmem_ld32(s_addr + 64 * half, x);
+    tmem_ld32(s_addr + 64 * half + 32, y);
+    tmem_ld_wait();
+    if (MASKED) {
+        const int left = lim - 64 * half;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            x[i] = i < left ? x[i] : -INFINITY;
+            y[i] = i + 32 < left ? y[i] : -INFINITY;
+        }
+    }
+}
+template <bool MASKED>
+__device__ __forceinline__ float row_max(unsigned s_addr, int lim)
+{
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+        float x[32], y[32];
+        load_scores<MASKED>(s_addr, half, lim, x, y);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mx[i & 3] = fmaxf(fmaxf(mx[i & 3], x[i]), y[i]);
+    }
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+}
+// The weights 2^(c s + base), written over the scores; returns their sum.
+template <bool MASKED, bool BF>
+__device__ __forceinline__ float row_weights(unsigned s_addr, int lim, float c, float base)
+{
+    const u64 c2 = pack2(c, c), base2 = pack2(base, base);
+    u64 sum2[2] = {0, 0};
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+        float x[32], y[32];
+        load_scores<MASKED>(s_addr, half, lim, x, y);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float y0, y1;
+                unpack2(ffma2(k ? pack2(y[2 * i], y[2 * i + 1]) : pack2(x[2 * i], x[2 * i + 1]), c2, base2), y0, y1);
+                y0 = exp2_fast(y0);
+                y1 = exp2_fast(y1);
+                sum2[i & 1] = fadd2(sum2[i & 1], pack2(y0, y1));
+                w[i] = pack16<BF>(y0, y1);
+            }
+            tmem_st16(s_addr + 32 * half + 16 * k, w);
+        }
+    }
+    sum2[0] = fadd2(sum2[0], sum2[1]);
+    return lo_of(sum2[0]) + hi_of(sum2[0]);
+}
+
+// A segment's tiles for the rows of row tile t.
+template <int TILES, bool BF>
+__device__ __forceinline__ void softmax_tiles(const ChunkParams &p, const Segment &sg, Shared<TILES> &sh, int cached, int sees, int t, unsigned turns, unsigned s_addr, unsigned o_addr, float &m, float &l)
+{
+    const float c = p.scale_log2;
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll 1
+    for (int j = 0; j < sg.n; ++j) {
+        const int tile = sg.ta + j, lim = tile < sg.ct ? cached - tile * T : sees - (tile - sg.ct) * T;
+        const bool masked = __any_sync(0xffffffffu, lim < T);
+        wait_for(sh.s_full[t], (turns + j) & 1, sh.failed, p.status);
+        tc_fence_after();
+        const float mx = c * (masked ? row_max<true>(s_addr, lim) : row_max<false>(s_addr, lim));
+        if (j == 0) m = mx;
+        else if (__any_sync(0xffffffffu, mx > m + GROW)) {
+            const float top = mx > m + GROW ? mx : m, use = top == -INFINITY ? 0.0f : top, f = exp2_fast(m - use);
+            m = top;
+            l *= f;
+#pragma unroll 1
+            for (int b = 0; b < 4; ++b) {
+                float x[32];
+                tmem_ld32(o_addr + 32 * b, x);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] *= f;
+                tmem_st32(o_addr + 32 * b, x);
+            }
+        }
+        const float base = P_SHIFT - (m == -INFINITY ? 0.0f : m);
+        l += masked ? row_weights<true, BF>(s_addr, lim, c, base) : row_weights<false, BF>(s_addr, lim, c, base);
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(smem_u32(&sh.p_full[t]));
+    }
+}
+
+template <int BITS, int TILES>
+__device__ __forceinline__ void softmax_role(const ChunkParams &p, Walk w, Shared<TILES> &sh, unsigned char *q_sm, unsigned tmem)
+{
+    using S = Plan<TILES>;
+    const int tid = threadIdx.x, warp = tid >> 5, t = warp / 4, r = tid;
+    unsigned turns = 0, segments = 0;                // scores of the row tile, and segments, so far
+    Segment sg;
+    while (walk_segment<S::ROWS>(p, w, sg)) {
+        for (bool bf = false;; bf = true) {
+            segment_begins(sh);
+            {
+                float top = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8];
+                    if (r < sg.n_rows) {
+                        const __nv_bfloat16 *from = p.q + (long long)(w.sq.q0 + (sg.row0 + r) / p.qpk) * p.qt + (long long)(w.pl.h * p.qpk + (sg.row0 + r) % p.qpk) * p.qh + 16 * u;
+                        const uint4 a = ldg128(from), b = ldg128(from + 8);
+                        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(bf16lo_to_f32(x[i])), fabsf(bf16hi_to_f32(x[i]))));
+                    unit_of_bf16<BITS>(x, bf, y);
+                    unsigned char *base = q_sm + r / 128 * OPERAND + u / 4 * (OPERAND / 2) + r % 128 * 128;
+                    *reinterpret_cast<uint4 *>(base + ((u % 4 * 2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<uint4 *>(base + (((u % 4 * 2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+                }
+                if (!(top < 4096.0f)) sh.wide = 1;
+                fence_async_smem();
+            }
+            __syncthreads();
+                const unsigned s_addr = tmem + 128 * t + ((unsigned)(warp % 4 * 32) << 16), o_addr = tmem + 128 * (TILES + t) + ((unsigned)(warp % 4 * 32) << 16);
+                const int sees = chunk_sees(p, w.sq, min(sg.row0 + r, sg.last) / p.qpk);
+                float m, l;
+                if (!bf) softmax_tiles<TILES, false>(p, sg, sh, w.sq.cached, sees, t, turns, s_addr, o_addr, m, l);
+                else softmax_tiles<TILES, true>(p, sg, sh, w.sq.cached, sees, t, turns, s_addr, o_addr, m, l);
+            wait_for(sh.o_full[t], segments & 1, sh.failed, p.status);
+            tc_fence_after();
+            if (!too_wide(sh, bf)) {                 // (known: the last tile was handed on after it)
+                    const bool whole = sg.ta == 0 && sg.tb == sg.tiles;
+                    const long long slot = 2LL * blockIdx.x + (sg.ta == 0 ? 1 : 0);
+                    const int row = sg.row0 + r, q_row = w.sq.q0 + row / p.qpk, hq = w.pl.h * p.qpk + row % p.qpk;
+                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                    const int odd_first = max(sh.odd_first, (max(sg.ta, sg.ct) - sg.ct) * T), odd_last = min(sh.odd_last, sees - 1);
+#pragma unroll 1
+                    for (int b = 0; b < 4; ++b) {
+                        float x[32];
+                        __syncwarp();
+                        tmem_ld32(o_addr + 32 * b, x);
+                        tmem_ld_wait();
+                        if (r >= sg.n_rows) continue;
+                        float y[32];                 // in the order of the channels
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const int e = i % 16, at_reg = BITS == 2 ? 2 * (e % 8) + e / 8 : e / 8 * 8 + 2 * (e % 4) + e % 8 / 4;
+                            y[i] = l == 0.0f ? 0.0f : x[i / 16 * 16 + at_reg];
+                        }
+                        for (int u = odd_first; u <= odd_last; ++u) {       // rare: infinities and NaN that the row sees
+                            const __nv_bfloat16 *v = p.v_new + (long long)(w.sq.k0 + u) * p.vnt + (long long)w.pl.h * p.vnh + 32 * b;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const float o = __bfloat162float(v[i]);
+                                if (!(fabsf(o) < INFINITY)) y[i] += o;
+                            }
+                        }
+                        if (whole) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w[i] = pack16<true>(y[2 * i] * inv, y[2 * i + 1] * inv);
+                            uint4 *to = reinterpret_cast<uint4 *>(p.out + (long long)q_row * p.ot + (long long)hq * p.oh + 32 * b);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) to[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                        } else {
+                            float4 *to = reinterpret_cast<float4 *>(p.part + (slot * S::ROWS + r) * D + 32 * b);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                        }
+                    }
+                    if (r < sg.n_rows) {
+                        if (!whole) *reinterpret_cast<float2 *>(p.ml + (slot * S::ROWS + r) * 2) = make_float2(m, l);
+                        else if (p.lse) p.lse[(long long)q_row * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
+                    }
+            }
+            tc_fence_before();
+            turns += sg.n;
+            ++segments;
+            if (!segment_again(sh, bf)) break;
+        }
+        walk_on<S::ROWS>(p, w, sg);
+    }
+}
+
+// A segment's tiles of keys and values.
+template <int BITS, int G, bool M16, int TILES, bool BF>
+__device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk &w, const Segment &sg, Shared<TILES> &sh, Producer<BITS, G, M16> &pr, int group32, unsigned kv,
+                                               unsigned char *k_sm, unsigned char *v_sm)
+{
+    using S = Plan<TILES>;
+    const int row0_sm = 32 * group32 + pr.sub;
+    // the first of the thread's 32 tokens of a tile in the pool; -1: past the cached tokens
+    auto place = [&](int t) -> long long {
+        const int tk = t * T + 32 * group32;
+        if (t >= min(sg.tb, sg.ct) || tk >= w.sq.cached) return -1;
+        const int pg = tk / p.pool.page_tokens;
+        int page = __ldg(p.page_table + (long long)w.pl.seq * p.table_stride + pg);
+        if ((unsigned)page >= (unsigned)p.pool.n_pages) {
+            atomicOr(p.status, SQUAT_FLAG_PAGES);
+            page = 0;
+        }
+        return (long long)page * p.pool.page_stride + (long long)w.pl.h * p.pool.head_stride + (tk - pg * p.pool.page_tokens);
+    };
+    __half2 ks_top = __float2half2_rn(0.0f), kz_top = ks_top, vs_top = ks_top, vz_top = ks_top;
+    float k_top = 0.0f, v_top = 0.0f;
+    // what the segment's magnitudes were: before the last tile is handed on, so that who waits for its sums knows them
+    auto publish = [&]() {
+        if (BF) return;
+        constexpr float L = float((1 << BITS) - 1);
+        auto top = [](__half2 x) { const float2 f = __half22float2(x); return fmaxf(f.x, f.y); };
+        atomicMax(&sh.k_top, __float_as_int(fmaxf(fmaf(L, top(ks_top), top(kz_top)), k_top)));
+        atomicMax(&sh.v_top, __float_as_int(fmaxf(fmaf(L, top(vs_top), top(vz_top)), v_top)));
+    };
+    long long tok = place(sg.ta), next = place(sg.ta + 1);
+    if (tok >= 0) {
+        pr.load_keys(p.pool, tok);
+        pr.load_values(p.pool, tok);
+    }
+#pragma unroll 1
+    for (int j = 0; j < sg.n; ++j) {
+        const int tile = sg.ta + j, stage = (kv + j) % S::STAGES;
+        const unsigned parity = (((kv + j) / S::STAGES) & 1) ^ 1;
+        unsigned char *k_to = k_sm + stage * OPERAND, *v_to = v_sm + stage * OPERAND;
+        if (tile < sg.ct) {
+            const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            wait_for(sh.k_empty[stage], parity, sh.failed, p.status);
+            if (tok >= 0) pr.template store_keys<BF>(k_to, row0_sm, ks_top, kz_top);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) store_unit(k_to, row0_sm + 4 * i, pr.unit, zero);         // behind the last cached token
+            fence_async_smem();
+            mbar_arrive(smem_u32(&sh.k_full[stage]));
+            if (next >= 0) pr.load_keys(p.pool, next);
+            wait_for(sh.v_empty[stage], parity, sh.failed, p.status);
+            if (tok >= 0) pr.template store_values<BF>(v_to, row0_sm, vs_top, vz_top);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) store_unit(v_to, row0_sm + 4 * i, pr.unit, zero);
+            if (j == sg.n - 1) publish();
+            fence_async_smem();
+            mbar_arrive(smem_u32(&sh.v_full[stage]));
+            if (next >= 0) pr.load_values(p.pool, next);
+            tok = next;
+            next = place(tile + 2);
+        } else {
+            // rows in full precision
+            const int u0 = (tile - sg.ct) * T + row0_sm;
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                const __nv_bfloat16 *src = side == 0 ? p.k_new : p.v_new;
+                const long long st = side == 0 ? p.knt : p.vnt, shd = side == 0 ? p.knh : p.vnh;
+                if (side == 0) wait_for(sh.k_empty[stage], parity, sh.failed, p.status);
+                else wait_for(sh.v_empty[stage], parity, sh.failed, p.status);
+#pragma unroll 2
+                for (int i = 0; i < 8; ++i) {
+                    const int u = u0 + 4 * i;
+                    uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8];
+                    if (u < sg.most) {
+                        const __nv_bfloat16 *from = src + (long long)(w.sq.k0 + u) * st + (long long)w.pl.h * shd + 16 * pr.unit;
+                        const uint4 a = ldg128(from), b = ldg128(from + 8);
+                        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+                    }
+                    bool odd = false;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (side == 1 && bf16_pair_not_finite(x[e])) {     // a row that does not see it must not meet it
+                            odd = true;
+                            if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+                            if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0x0000ffffu;
+                        }
+                        const float lo = fabsf(bf16lo_to_f32(x[e])), hi = fabsf(bf16hi_to_f32(x[e]));
+                        if (side == 0) k_top = fmaxf(k_top, fmaxf(lo < INFINITY ? lo : 0.0f, hi < INFINITY ? hi : 0.0f));
+                        else v_top = fmaxf(v_top, fmaxf(lo, hi));
+                    }
+                    if (odd) {
+                        atomicMin(&sh.odd_first, u);
+                        atomicMax(&sh.odd_last, u);
+                    }
+                    unit_of_bf16<BITS>(x, BF, y);
+                    store_unit(side == 0 ? k_to : v_to, row0_sm + 4 * i, pr.unit, y);
+                }
+                if (side == 1 && j == sg.n - 1) publish();
+                fence_async_smem();
+                mbar_arrive(smem_u32(side == 0 ? &sh.k_full[stage] : &sh.v_full[stage]));
+            }
+        }
+    }
+}
+
+template <int BITS, int G, bool M16, int TILES>
+__device__ __forceinline__ void producer_role(const ChunkParams &p, Walk w, Shared<TILES> &sh, unsigned char *k_sm, unsigned char *v_sm)
+{
+    using S = Plan<TILES>;
+    const int pt = threadIdx.x - S::SOFT, group32 = pt / 32;
+    Producer<BITS, G, M16> pr;
+    pr.sub = pt / 8 % 4;
+    pr.unit = pt % 8;
+    unsigned kv = 0;                                 // tiles so far
+    Segment sg;
+    while (walk_segment<S::ROWS>(p, w, sg)) {
+        for (bool bf = false;; bf = true) {
+            segment_begins(sh);
+            __syncthreads();
+            {
+                if (!bf) producer_tiles<BITS, G, M16, TILES, false>(p, w, sg, sh, pr, group32, kv, k_sm, v_sm);
+                else producer_tiles<BITS, G, M16, TILES, true>(p, w, sg, sh, pr, group32, kv, k_sm, v_sm);
+            }
+            kv += sg.n;
+            if (!segment_again(sh, bf)) break;
+        }
+        walk_on<S::ROWS>(p, w, sg);
+    }
+}
+
+template <int TILES>
+__device__ __forceinline__ void product_role(const ChunkParams &p, Walk w, Shared<TILES> &sh, unsigned char *q_sm, unsigned char *k_sm, unsigned char *v_sm, unsigned tmem, bool issues)
+{
+    using S = Plan<TILES>;
+    unsigned kv = 0, turns = 0;
+    Segment sg;
+    while (walk_segment<S::ROWS>(p, w, sg)) {
+        for (bool bf = false;; bf = true) {
+            segment_begins(sh);
+            __syncthreads();
+            if (issues) {
+                const unsigned id_s = idesc_16(bf, false), id_o = idesc_16(bf, true);
+                auto scores = [&](int t, int stage) {
+                    const u64 a = rows_desc(smem_u32(q_sm + t * OPERAND)), b = rows_desc(smem_u32(k_sm + stage * OPERAND));
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const int off = (s / 4 * (OPERAND / 2) + s % 4 * 32) >> 4;
+                        mma_ss(tmem + 128 * t, a + off, b + off, id_s, s > 0);
+                    }
+                };
+                wait_for(sh.k_full[kv % S::STAGES], (kv / S::STAGES) & 1, sh.failed, p.status);
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        scores(t, kv % S::STAGES);
+                        tc_commit(smem_u32(&sh.s_full[t]));
+                    }
+                    tc_commit(smem_u32(&sh.k_empty[kv % S::STAGES]));
+                }
+                __syncwarp();
+#pragma unroll 1
+                for (int j = 0; j < sg.n; ++j) {
+                    const int stage = (kv + j) % S::STAGES, next = (kv + j + 1) % S::STAGES;
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) {
+                        if (t == 0) wait_for(sh.v_full[stage], ((kv + j) / S::STAGES) & 1, sh.failed, p.status);
+                        wait_for(sh.p_full[t], (turns + j) & 1, sh.failed, p.status);
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const u64 b = columns_desc(smem_u32(v_sm + stage * OPERAND));
+#pragma unroll
+                            for (int s = 0; s < 8; ++s) mma_ts(tmem + 128 * (TILES + t), tmem + 128 * t + 8 * s, b + (s * 2048 >> 4), id_o, j > 0 || s > 0);
+                            if (t == TILES - 1) tc_commit(smem_u32(&sh.v_empty[stage]));
+                            if (j + 1 == sg.n) tc_commit(smem_u32(&sh.o_full[t]));
+                        }
+                        __syncwarp();
+                        if (j + 1 == sg.n) continue;
+                        if (t == 0) {
+                            wait_for(sh.k_full[next], ((kv + j + 1) / S::STAGES) & 1, sh.failed, p.status);
+                            tc_fence_after();
+                        }
+                        if (elect_one()) {
+                            scores(t, next);
+                            tc_commit(smem_u32(&sh.s_full[t]));
+                            if (t == TILES - 1) tc_commit(smem_u32(&sh.k_empty[next]));
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+            kv += sg.n;
+            turns += sg.n;
+            if (!segment_again(sh, bf)) break;
+        }
+        walk_on<S::ROWS>(p, w, sg);
+    }
+}
 
 template <int BITS, int G, bool M16, int TILES>
 __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk_matrix_kernel(const __grid_constant__ ChunkParams params)
 {
     using S = Plan<TILES>;
-    using Pr = Producer<BITS, G, M16, TILES>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared<TILES> sh;
     unsigned char *q_sm = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024, *k_sm = q_sm + TILES * OPERAND, *v_sm = k_sm + S::STAGES * OPERAND;
@@ -181,12 +714,13 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
     grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
     long long per, total;
     chunk_share<S::ROWS, T>(p, sh.place, per, total);
-    long long at = per * blockIdx.x;
-    if (at >= total) return;
-    const long long end = min(at + per, total);
-    chunk_locate<S::ROWS, T, 1>(p, sh.place, at, per);
-    ChunkPlace pl = sh.place.found[0];
-    ChunkSeq sq = chunk_seq(p, pl.seq);
+    Walk w;
+    w.at = per * blockIdx.x;
+    if (w.at >= total) return;
+    w.end = min(w.at + per, total);
+    chunk_locate<S::ROWS, T, 1>(p, sh.place, w.at, per);
+    w.pl = sh.place.found[0];
+    w.sq = chunk_seq(p, w.pl.seq);
     if (warp == MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"((unsigned)S::TMEM) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -210,385 +744,16 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
     __syncthreads();
     tc_fence_after();
     const unsigned tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
-    unsigned kv = 0, turns = 0, segments = 0;        // tiles of tokens, scores of a row tile, and segments so far
-
-    while (at < end) {
-        const int tiles = chunk_tiles<S::ROWS, T>(p, sq, pl.qt), begin = pl.at, stop = (int)min((long long)p.start + tiles, begin + (end - at));
-        const int ta = max(begin - p.start, 0), tb = max(stop - p.start, 0), n = tb - ta;
-        const int rows = sq.nq * p.qpk, row0 = pl.qt * S::ROWS, n_rows = min(S::ROWS, rows - row0), last = row0 + n_rows - 1;
-        const int ct = (sq.cached + T - 1) / T, most = chunk_sees(p, sq, last / p.qpk);
-        bool bf = false;
-        while (n > 0) {
-            if (tid == 0) {
-                sh.wide = 0;
-                sh.odd_first = 0x7fffffff;
-                sh.odd_last = -1;
-                sh.v_top = sh.k_top = 0;
-            }
-            __syncthreads();
-            // ---------------------------------------------------------------- queries, a thread a row
-            if (tid < S::SOFT) {
-                const int r = tid;
-                float top = 0.0f;
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8];
-                    if (r < n_rows) {
-                        const __nv_bfloat16 *from = p.q + (long long)(sq.q0 + (row0 + r) / p.qpk) * p.qt + (long long)(pl.h * p.qpk + (row0 + r) % p.qpk) * p.qh + 16 * u;
-                        const uint4 a = ldg128(from), b = ldg128(from + 8);
-                        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(bf16lo_to_f32(x[i])), fabsf(bf16hi_to_f32(x[i]))));
-                    unit_of_bf16<BITS>(x, bf, y);
-                    unsigned char *base = q_sm + r / 128 * OPERAND + u / 4 * (OPERAND / 2) + r % 128 * 128;
-                    *reinterpret_cast<uint4 *>(base + ((u % 4 * 2 ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                    *reinterpret_cast<uint4 *>(base + (((u % 4 * 2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
-                }
-                if (!(top < 4096.0f)) sh.wide = 1;
-                fence_async_smem();
-            }
-            __syncthreads();
-
-            if (warp < SOFT_WARPS) {
-                // ------------------------------------------------------------ softmax
-                const int t = warp / 4, r = tid;
-                const unsigned s_addr = tmem + 128 * t + ((unsigned)(warp % 4 * 32) << 16), o_addr = tmem + 128 * (TILES + t) + ((unsigned)(warp % 4 * 32) << 16);
-                const int sees = chunk_sees(p, sq, min(row0 + r, last) / p.qpk);
-                float m = -INFINITY, l = 0.0f;
-                const float c = p.scale_log2;
-#pragma unroll 1
-                for (int j = 0; j < n; ++j) {
-                    const int tile = ta + j, lim = tile < ct ? sq.cached - tile * T : sees - (tile - ct) * T;
-                    const bool masked = __any_sync(0xffffffffu, lim < T);
-                    wait_for(sh.s_full[t], (turns + j) & 1, sh.failed, p.status);
-                    tc_fence_after();
-                    float x[32], mx = -INFINITY;
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        tmem_ld32(s_addr + 32 * b, x);
-                        tmem_ld_wait();
-                        if (masked)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = 32 * b + i < lim ? x[i] : -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, x[i]);
-                    }
-                    mx *= c;
-                    if (j == 0) m = mx;
-                    else if (__any_sync(0xffffffffu, mx > m + GROW)) {
-                        const float top = mx > m + GROW ? mx : m, use = top == -INFINITY ? 0.0f : top, f = exp2_fast(m - use);
-                        m = top;
-                        l *= f;
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) {
-                            tmem_ld32(o_addr + 32 * b, x);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] *= f;
-                            tmem_st32(o_addr + 32 * b, x);
-                        }
-                    }
-                    const float base = P_SHIFT - (m == -INFINITY ? 0.0f : m);
-                    const u64 c2 = pack2(c, c), base2 = pack2(base, base);
-                    u64 sum2 = 0;
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        tmem_ld32(s_addr + 32 * b, x);
-                        tmem_ld_wait();
-                        if (masked)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = 32 * b + i < lim ? x[i] : -INFINITY;
-                        uint32_t w[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            float y0, y1;
-                            unpack2(ffma2(pack2(x[2 * i], x[2 * i + 1]), c2, base2), y0, y1);
-                            y0 = exp2_fast(y0);
-                            y1 = exp2_fast(y1);
-                            sum2 = fadd2(sum2, pack2(y0, y1));
-                            w[i] = bf ? pack16<true>(y0, y1) : pack16<false>(y0, y1);
-                        }
-                        tmem_st16(s_addr + 16 * b, w);
-                    }
-                    l += lo_of(sum2) + hi_of(sum2);
-                    tmem_st_wait();
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&sh.p_full[t]));
-                }
-                wait_for(sh.o_full[t], segments & 1, sh.failed, p.status);
-                tc_fence_after();
-                // ------------------------------------------------------------ result: of the segment (`wide` and the values' range are known)
-                const float v_top = __int_as_float(*(volatile int *)&sh.v_top);
-                const bool again = !bf && (*(volatile int *)&sh.wide || !(__int_as_float(*(volatile int *)&sh.k_top) < 4096.0f) || !(v_top < 65000.0f) || (v_top < 0x1p-8f && v_top > 0.0f));
-                if (!again) {
-                    const bool whole = ta == 0 && tb == tiles;
-                    const long long slot = 2LL * blockIdx.x + (ta == 0 ? 1 : 0);
-                    const int row = row0 + r, q_row = sq.q0 + row / p.qpk, hq = pl.h * p.qpk + row % p.qpk;
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                    const int odd_first = max(sh.odd_first, (max(ta, ct) - ct) * T), odd_last = min(sh.odd_last, sees - 1);
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        float x[32];
-                        __syncwarp();
-                        tmem_ld32(o_addr + 32 * b, x);
-                        tmem_ld_wait();
-                        if (r >= n_rows) continue;
-                        float y[32];                 // in the order of the channels
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const int e = i % 16, at_reg = BITS == 2 ? 2 * (e % 8) + e / 8 : e / 8 * 8 + 2 * (e % 4) + e % 8 / 4;
-                            y[i] = l == 0.0f ? 0.0f : x[i / 16 * 16 + at_reg];
-                        }
-                        for (int u = odd_first; u <= odd_last; ++u) {       // rare: infinities and NaN that the row sees
-                            const __nv_bfloat16 *v = p.v_new + (long long)(sq.k0 + u) * p.vnt + (long long)pl.h * p.vnh + 32 * b;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                const float o = __bfloat162float(v[i]);
-                                if (!(fabsf(o) < INFINITY)) y[i] += o;
-                            }
-                        }
-                        if (whole) {
-                            uint32_t w[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = pack16<true>(y[2 * i] * inv, y[2 * i + 1] * inv);
-                            uint4 *to = reinterpret_cast<uint4 *>(p.out + (long long)q_row * p.ot + (long long)hq * p.oh + 32 * b);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) to[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-                        } else {
-                            float4 *to = reinterpret_cast<float4 *>(p.part + (slot * S::ROWS + r) * D + 32 * b);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-                        }
-                    }
-                    if (r < n_rows) {
-                        if (!whole) *reinterpret_cast<float2 *>(p.ml + (slot * S::ROWS + r) * 2) = make_float2(m, l);
-                        else if (p.lse) p.lse[(long long)q_row * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
-                    }
-                }
-                tc_fence_before();
-            } else if (warp < MMA_WARP) {
-                // ------------------------------------------------------------ producers
-                const int pt = tid - S::SOFT;
-                const CodeBias<BITS> bias;
-                const Pr pr{p, sq, bias, pl.h, most, ct, pt / 32, pt / 8 % 4, pt % 8};
-                const int row0_sm = 32 * pr.group32 + pr.sub;
-                __half2 ks_top = __float2half2_rn(0.0f), kz_top = ks_top, vs_top = ks_top, vz_top = ks_top;
-                float k_top = 0.0f, v_top = 0.0f;
-                // what the segment's magnitudes were: before the last tile is handed on, so that who waits for its sums knows them
-                auto publish = [&]() {
-                    if (bf) return;
-                    constexpr float L = float((1 << BITS) - 1);
-                    auto top = [](__half2 x) { const float2 f = __half22float2(x); return fmaxf(f.x, f.y); };
-                    atomicMax(&sh.k_top, __float_as_int(fmaxf(fmaf(L, top(ks_top), top(kz_top)), k_top)));
-                    atomicMax(&sh.v_top, __float_as_int(fmaxf(fmaf(L, top(vs_top), top(vz_top)), v_top)));
-                };
-                long long next = pr.place(pl.seq, ta);
-#pragma unroll 1
-                for (int j = 0; j < n; ++j) {
-                    const int tile = ta + j, stage = (kv + j) % S::STAGES;
-                    const unsigned parity = (((kv + j) / S::STAGES) & 1) ^ 1;
-                    unsigned char *k_to = k_sm + stage * OPERAND, *v_to = v_sm + stage * OPERAND;
-                    const long long tok = next;
-                    if (j + 1 < n) next = pr.place(pl.seq, tile + 1);
-                    if (tile < ct) {
-                        Units<BITS> ku, vu;
-                        float sc[16], zr[16], vsc[8], vzr[8];
-                        if (tok >= 0) {
-                            pr.load_codes(p.pool.kc, tok, ku);
-                            const long long mk = tok / G * D + 16 * pr.unit;
-                            if (M16) {
-#pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    const uint4 a = ldg128(static_cast<const __half *>(p.pool.ks) + mk + 8 * i), b = ldg128(static_cast<const __half *>(p.pool.kz) + mk + 8 * i);
-                                    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        const float2 u = __half22float2(as_half2(aw[e])), v = __half22float2(as_half2(bw[e]));
-                                        sc[8 * i + 2 * e] = u.x; sc[8 * i + 2 * e + 1] = u.y;
-                                        zr[8 * i + 2 * e] = v.x; zr[8 * i + 2 * e + 1] = v.y;
-                                    }
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    *reinterpret_cast<float4 *>(sc + 4 * i) = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(p.pool.ks) + mk) + i);
-                                    *reinterpret_cast<float4 *>(zr + 4 * i) = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(p.pool.kz) + mk) + i);
-                                }
-                            }
-                            pr.load_codes(p.pool.vc, tok, vu);
-                            const long long mv = (tok + pr.sub) * Pr::NG + 16 * pr.unit / G;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                vsc[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(p.pool.vs) + mv + 4 * i * Pr::NG)) : __ldg(static_cast<const float *>(p.pool.vs) + mv + 4 * i * Pr::NG);
-                                vzr[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(p.pool.vz) + mv + 4 * i * Pr::NG)) : __ldg(static_cast<const float *>(p.pool.vz) + mv + 4 * i * Pr::NG);
-                            }
-                        }
-                        wait_for(sh.k_empty[stage], parity, sh.failed, p.status);
-                        if (tok < 0) {               // behind the last cached token: zeros
-                            const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) store_unit(k_to, row0_sm + 4 * i, pr.unit, zero);
-                        } else if (!bf) {
-                            __half2 s2[8], z2[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                s2[e] = __floats2half2_rn(sc[Pr::lo_of_reg(e)], sc[Pr::hi_of_reg(e)]);
-                                z2[e] = __floats2half2_rn(zr[Pr::lo_of_reg(e)], zr[Pr::hi_of_reg(e)]);
-                                ks_top = __hmax2(ks_top, __habs2(s2[e]));
-                                kz_top = __hmax2(kz_top, __habs2(z2[e]));
-                            }
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                uint32_t y[8];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(pr.pair(ku, i, e), s2[e], z2[e]));
-                                store_unit(k_to, row0_sm + 4 * i, pr.unit, y);
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                uint32_t y[8];
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const int a = Pr::lo_of_reg(e), b = Pr::hi_of_reg(e);
-                                    y[e] = pack16<true>(fmaf(Pr::code_at(ku, i, a), sc[a], zr[a]), fmaf(Pr::code_at(ku, i, b), sc[b], zr[b]));
-                                }
-                                store_unit(k_to, row0_sm + 4 * i, pr.unit, y);
-                            }
-                        }
-                        fence_async_smem();
-                        mbar_arrive(smem_u32(&sh.k_full[stage]));
-                        wait_for(sh.v_empty[stage], parity, sh.failed, p.status);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            uint32_t y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                            if (tok >= 0) {
-                                const __half2 s2 = __float2half2_rn(vsc[i]), z2 = __float2half2_rn(vzr[i]);
-                                if (!bf) {
-                                    vs_top = __hmax2(vs_top, __habs2(s2));
-                                    vz_top = __hmax2(vz_top, __habs2(z2));
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e) y[e] = as_u32(__hfma2(pr.pair(vu, i, e), s2, z2));
-                                } else {
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e)
-                                        y[e] = pack16<true>(fmaf(Pr::code_at(vu, i, Pr::lo_of_reg(e)), vsc[i], vzr[i]), fmaf(Pr::code_at(vu, i, Pr::hi_of_reg(e)), vsc[i], vzr[i]));
-                                }
-                            }
-                            store_unit(v_to, row0_sm + 4 * i, pr.unit, y);
-                        }
-                        if (j == n - 1) publish();
-                        fence_async_smem();
-                        mbar_arrive(smem_u32(&sh.v_full[stage]));
-                    } else {
-                        // rows in full precision
-                        const int u0 = (tile - ct) * T + row0_sm;
-#pragma unroll
-                        for (int side = 0; side < 2; ++side) {
-                            const __nv_bfloat16 *src = side == 0 ? p.k_new : p.v_new;
-                            const long long st = side == 0 ? p.knt : p.vnt, shd = side == 0 ? p.knh : p.vnh;
-                            if (side == 0) wait_for(sh.k_empty[stage], parity, sh.failed, p.status);
-                            else wait_for(sh.v_empty[stage], parity, sh.failed, p.status);
-#pragma unroll 2
-                            for (int i = 0; i < 8; ++i) {
-                                const int u = u0 + 4 * i;
-                                uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8];
-                                if (u < most) {
-                                    const __nv_bfloat16 *from = src + (long long)(sq.k0 + u) * st + (long long)pl.h * shd + 16 * pr.unit;
-                                    const uint4 a = ldg128(from), b = ldg128(from + 8);
-                                    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-                                }
-                                bool odd = false;
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    if (side == 1 && bf16_pair_not_finite(x[e])) {     // a row that does not see it must not meet it
-                                        odd = true;
-                                        if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
-                                        if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0x0000ffffu;
-                                    }
-                                    const float lo = fabsf(bf16lo_to_f32(x[e])), hi = fabsf(bf16hi_to_f32(x[e]));
-                                    if (side == 0) k_top = fmaxf(k_top, fmaxf(lo < INFINITY ? lo : 0.0f, hi < INFINITY ? hi : 0.0f));
-                                    else v_top = fmaxf(v_top, fmaxf(lo, hi));
-                                }
-                                if (odd) {
-                                    atomicMin(&sh.odd_first, u);
-                                    atomicMax(&sh.odd_last, u);
-                                }
-                                unit_of_bf16<BITS>(x, bf, y);
-                                store_unit(side == 0 ? k_to : v_to, row0_sm + 4 * i, pr.unit, y);
-                            }
-                            if (side == 1 && j == n - 1) publish();
-                            fence_async_smem();
-                            mbar_arrive(smem_u32(side == 0 ? &sh.k_full[stage] : &sh.v_full[stage]));
-                        }
-                    }
-                }
-            } else {
-                // ------------------------------------------------------------ products
-                const unsigned id_s = idesc_16(bf, false), id_o = idesc_16(bf, true);
-                auto scores = [&](int t, int stage) {
-                    const u64 a = rows_desc(smem_u32(q_sm + t * OPERAND)), b = rows_desc(smem_u32(k_sm + stage * OPERAND));
-#pragma unroll
-                    for (int s = 0; s < 8; ++s) {
-                        const int off = (s / 4 * (OPERAND / 2) + s % 4 * 32) >> 4;
-                        mma_ss(tmem + 128 * t, a + off, b + off, id_s, s > 0);
-                    }
-                };
-                wait_for(sh.k_full[kv % S::STAGES], (kv / S::STAGES) & 1, sh.failed, p.status);
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) {
-                        scores(t, kv % S::STAGES);
-                        tc_commit(smem_u32(&sh.s_full[t]));
-                    }
-                    tc_commit(smem_u32(&sh.k_empty[kv % S::STAGES]));
-                }
-                __syncwarp();
-#pragma unroll 1
-                for (int j = 0; j < n; ++j) {
-                    const int stage = (kv + j) % S::STAGES, next = (kv + j + 1) % S::STAGES;
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) {
-                        if (t == 0) wait_for(sh.v_full[stage], ((kv + j) / S::STAGES) & 1, sh.failed, p.status);
-                        wait_for(sh.p_full[t], (turns + j) & 1, sh.failed, p.status);
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const u64 b = columns_desc(smem_u32(v_sm + stage * OPERAND));
-#pragma unroll
-                            for (int s = 0; s < 8; ++s) mma_ts(tmem + 128 * (TILES + t), tmem + 128 * t + 8 * s, b + (s * 2048 >> 4), id_o, j > 0 || s > 0);
-                            if (t == TILES - 1) tc_commit(smem_u32(&sh.v_empty[stage]));
-                            if (j + 1 == n) tc_commit(smem_u32(&sh.o_full[t]));
-                        }
-                        __syncwarp();
-                        if (j + 1 == n) continue;
-                        if (t == 0) {
-                            wait_for(sh.k_full[next], ((kv + j + 1) / S::STAGES) & 1, sh.failed, p.status);
-                            tc_fence_after();
-                        }
-                        if (elect_one()) {
-                            scores(t, next);
-                            tc_commit(smem_u32(&sh.s_full[t]));
-                            if (t == TILES - 1) tc_commit(smem_u32(&sh.k_empty[next]));
-                        }
-                        __syncwarp();
-                    }
-                }
-            }
-            kv += n;
-            turns += n;
-            ++segments;
-            __syncthreads();                         // (and the sums have been read)
-            tc_fence_after();
-            const float v_top = __int_as_float(sh.v_top);
-            const bool again = !bf && (sh.wide || !(__int_as_float(sh.k_top) < 4096.0f) || !(v_top < 65000.0f) || (v_top < 0x1p-8f && v_top > 0.0f));
-            __syncthreads();
-            if (!again) break;
-            bf = true;
-        }
-        at += stop - begin;
-        if (at < end) chunk_next<S::ROWS>(p, pl, sq);
+    // registers: the three roles' shares add up to what the block was launched with
+    if (warp < SOFT_WARPS) {
+        more_registers<S::SOFT_REGS>();
+        softmax_role<BITS, TILES>(p, w, sh, q_sm, tmem);
+    } else if (warp < MMA_WARP) {
+        more_registers<S::PRODUCER_REGS>();
+        producer_role<BITS, G, M16, TILES>(p, w, sh, k_sm, v_sm);
+    } else {
+        fewer_registers<S::PRODUCT_REGS>();
+        product_role<TILES>(p, w, sh, q_sm, k_sm, v_sm, tmem, warp == MMA_WARP);
     }
     tc_fence_before();
     __syncthreads();
@@ -600,7 +765,13 @@ int launch_matrix(const ChunkParams &p, cudaStream_t st)
 {
     using S = Plan<TILES>;
     static std::atomic<unsigned long long> allowed{0};
-    const int rc = squat_allow_smem(reinterpret_cast<const void *>(chunk_matrix_kernel<BITS, G, M16, TILES>), S::SMEM, allowed);
+    const void *kernel = reinterpret_cast<const void *>(chunk_matrix_kernel<BITS, G, M16, TILES>);
+    if (!allowed.load(std::memory_order_acquire)) {  // the roles' registers are taken out of the block's: a build with fewer would wait for them for good
+        cudaFuncAttributes a;
+        SQUAT_CUDA(cudaFuncGetAttributes(&a, kernel));
+        if (a.numRegs != S::LAUNCH_REGS) return SQUAT_ERR_UNSUPPORTED;
+    }
+    const int rc = squat_allow_smem(kernel, S::SMEM, allowed);
     if (rc != SQUAT_OK) return rc;
     return squat_launch(chunk_matrix_kernel<BITS, G, M16, TILES>, p.n_workers, S::THREADS, S::SMEM, st, p);
 }
