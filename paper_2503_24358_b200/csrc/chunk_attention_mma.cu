@@ -3,8 +3,8 @@
 //
 // An item is 128 or 256 rows (TILES tiles of 128) of one KV head.  Roles of a CTA's warps, handing tiles of 128 tokens on through
 // mbarriers:
-//   producers (4 warps)  dequantize keys and values into shared memory, binary16 in the 128-byte swizzle, once for all rows of the
-//                        item: a thread takes 16 channels of a token, eight tokens of one group of keys, whose scales it holds.
+//   producers (8 warps)  dequantize keys and values into shared memory, binary16 in the 128-byte swizzle, once for all rows of the
+//                        item: a thread takes 16 channels of four tokens of one group of keys, whose scales it holds.
 //   products (1 thread)  S = Q K^T into tensor memory, then O += P V with P taken from tensor memory; per tile of rows in the order
 //                        PV(j), QK(j + 1), so that the scores of one tile are made while the other tile's warps work on theirs.
 //   softmax (4 warps a tile)  a thread owns a row: maximum, weights 2^(c s - m + 8), written over its scores as binary16, and the
@@ -23,12 +23,12 @@ constexpr int OPERAND = T * D * 2;                   // bytes of a tile of 128 r
 
 template <int TILES>
 struct Plan {
-    static constexpr int ROWS = 128 * TILES, STAGES = TILES, SOFT = 128 * TILES, THREADS = SOFT + 256;
+    static constexpr int ROWS = 128 * TILES, STAGES = TILES, SOFT = 128 * TILES, PRODUCERS = 256, THREADS = SOFT + PRODUCERS + 128;
     static constexpr int CTAS = TILES == 2 ? 1 : 2;  // to an SM
     static constexpr int TMEM = 256 * TILES;         // columns: scores (and weights) of each tile, then sums of each tile
     // registers of a thread at launch, and of the roles' threads after it
-    static constexpr int LAUNCH_REGS = TILES == 2 ? 128 : 80, SOFT_REGS = TILES == 2 ? 144 : 96, PRODUCER_REGS = TILES == 2 ? 160 : 112, PRODUCT_REGS = TILES == 2 ? 64 : 32;
-    static_assert(TILES * SOFT_REGS + PRODUCER_REGS + PRODUCT_REGS == (TILES + 2) * LAUNCH_REGS, "more registers than the block is launched with");
+    static constexpr int LAUNCH_REGS = TILES == 2 ? 96 : 64, SOFT_REGS = TILES == 2 ? 136 : 96, PRODUCER_REGS = TILES == 2 ? 80 : 64, PRODUCT_REGS = TILES == 2 ? 48 : 32;
+    static_assert(TILES * SOFT_REGS + 2 * PRODUCER_REGS + PRODUCT_REGS == (TILES + 3) * LAUNCH_REGS, "more registers than the block is launched with");
     static constexpr size_t SMEM = 1024 + (size_t)(TILES + 2 * STAGES) * OPERAND;
 };
 
@@ -98,15 +98,13 @@ __device__ __forceinline__ void wait_for(u64 &bar, unsigned parity, int &failed,
     atomicOr(status, SQUAT_FLAG_DEVICE_TIMEOUT);
 }
 
-// 16 channels of a token in the operand: two 16-byte pieces.  Lanes of the upper half store the second one first, so that eight lanes
-// of a token fall on distinct banks.
+// 16 channels of a token in the operand: two 16-byte pieces.  (Eight lanes hold four units of two neighbouring tokens: distinct banks.)
 __device__ __forceinline__ void store_unit(unsigned char *operand, int row, int unit, const uint32_t (&r)[8])
 {
     unsigned char *base = operand + unit / 4 * (OPERAND / 2) + row * 128;
-    const int c = unit % 4 * 2, first = unit / 4;
-    const uint4 a = make_uint4(r[0], r[1], r[2], r[3]), b = make_uint4(r[4], r[5], r[6], r[7]);
-    *reinterpret_cast<uint4 *>(base + (((c + first) ^ (row & 7)) << 4)) = first ? b : a;
-    *reinterpret_cast<uint4 *>(base + (((c + 1 - first) ^ (row & 7)) << 4)) = first ? a : b;
+    const int c = unit % 4 * 2 ^ (row & 7);
+    *reinterpret_cast<uint4 *>(base + (c << 4)) = make_uint4(r[0], r[1], r[2], r[3]);
+    *reinterpret_cast<uint4 *>(base + ((c ^ 1) << 4)) = make_uint4(r[4], r[5], r[6], r[7]);
 }
 
 // 16 bf16 numbers, as loaded, in the operand's order
@@ -120,26 +118,26 @@ __device__ __forceinline__ void unit_of_bf16(const uint32_t (&x)[8], bool bf, ui
     }
 }
 
-// A producer's part of a tile of cached tokens: tokens 32 (thread / 32) + thread / 8 mod 4 + 4 i (one page, one group of keys), channels
-// 16 (thread mod 8) .. + 15.  Keys and values are asked for a tile ahead: the keys of the next tile while this one's values are made, and
-// the other way round.
+// A producer's part of a tile of cached tokens: four tokens, eight apart, of 32 (one page, one group of keys), 16 channels each.  Keys
+// and values are asked for a tile ahead: the keys of the next tile while this one's values are made, and the other way round.
+constexpr int UNITS = 4, APART = 8;
 template <int BITS, int G, bool M16>
 struct Producer {
     static constexpr int ROW = D * BITS / 8, NG = D / G;
     const CodeBias<BITS> bias;
-    int sub, unit;                                   // thread / 8 mod 4, thread mod 8
-    uint32_t code[2][8][BITS / 2];                   // keys, values
+    int sub, unit;                                   // the first of its tokens, its channels
+    uint32_t code[2][UNITS][BITS / 2];                   // keys, values
     uint4 ks[M16 ? 2 : 4], kz[M16 ? 2 : 4];          // the unit's scales and zero-points (keys)
-    float vs[8], vz[8];                              // the tokens' (values)
+    float vs[UNITS], vz[UNITS];                              // the tokens' (values)
 
     __device__ __forceinline__ void load_codes(int side, const unsigned char *codes, long long tok)
     {
         const unsigned char *from = codes + (tok + sub) * ROW + unit * (2 * BITS);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (BITS == 2) code[side][i][0] = __ldg(reinterpret_cast<const uint32_t *>(from + 4 * i * ROW));
+        for (int i = 0; i < UNITS; ++i) {
+            if (BITS == 2) code[side][i][0] = __ldg(reinterpret_cast<const uint32_t *>(from + APART * i * ROW));
             else {
-                const uint2 v = __ldg(reinterpret_cast<const uint2 *>(from + 4 * i * ROW));
+                const uint2 v = __ldg(reinterpret_cast<const uint2 *>(from + APART * i * ROW));
                 code[side][i][0] = v.x; code[side][i][BITS / 2 - 1] = v.y;
             }
         }
@@ -159,9 +157,9 @@ struct Producer {
         load_codes(1, pool.vc, tok);
         const long long at = (tok + sub) * NG + 16 * unit / G;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            vs[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(pool.vs) + at + 4 * i * NG)) : __ldg(static_cast<const float *>(pool.vs) + at + 4 * i * NG);
-            vz[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(pool.vz) + at + 4 * i * NG)) : __ldg(static_cast<const float *>(pool.vz) + at + 4 * i * NG);
+        for (int i = 0; i < UNITS; ++i) {
+            vs[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(pool.vs) + at + APART * i * NG)) : __ldg(static_cast<const float *>(pool.vs) + at + APART * i * NG);
+            vz[i] = M16 ? __half2float(__ldg(static_cast<const __half *>(pool.vz) + at + APART * i * NG)) : __ldg(static_cast<const float *>(pool.vz) + at + APART * i * NG);
         }
     }
     // register m of a unit holds channels lo_of(m) and lo_of(m) + HALF
@@ -204,22 +202,22 @@ struct Producer {
                 z_top = __hmax2(z_top, __habs2(z2[m]));
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < UNITS; ++i) {
                 uint32_t y[8];
 #pragma unroll
                 for (int m = 0; m < 8; ++m) y[m] = as_u32(__hfma2(pair(0, i, m), s2[m], z2[m]));
-                store_unit(to, row + 4 * i, unit, y);
+                store_unit(to, row + APART * i, unit, y);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < UNITS; ++i) {
                 uint32_t y[8];
 #pragma unroll
                 for (int m = 0; m < 8; ++m) {
                     const int lo = lo_of(m), hi = lo + HALF;
                     y[m] = pack16<true>(fmaf(code_at(0, i, lo), meta(ks, lo), meta(kz, lo)), fmaf(code_at(0, i, hi), meta(ks, hi), meta(kz, hi)));
                 }
-                store_unit(to, row + 4 * i, unit, y);
+                store_unit(to, row + APART * i, unit, y);
             }
         }
     }
@@ -227,7 +225,7 @@ struct Producer {
     __device__ __forceinline__ void store_values(unsigned char *to, int row, __half2 &s_top, __half2 &z_top) const
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < UNITS; ++i) {
             uint32_t y[8];
             if (!BF) {
                 const __half2 s2 = __float2half2_rn(vs[i]), z2 = __float2half2_rn(vz[i]);
@@ -239,7 +237,7 @@ struct Producer {
 #pragma unroll
                 for (int m = 0; m < 8; ++m) y[m] = pack16<true>(fmaf(code_at(1, i, lo_of(m)), vs[i], vz[i]), fmaf(code_at(1, i, lo_of(m) + HALF), vs[i], vz[i]));
             }
-            store_unit(to, row + 4 * i, unit, y);
+            store_unit(to, row + APART * i, unit, y);
         }
     }
 };
@@ -547,7 +545,7 @@ __device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk 
             if (tok >= 0) pr.template store_keys<BF>(k_to, row0_sm, ks_top, kz_top);
             else
 #pragma unroll
-                for (int i = 0; i < 8; ++i) store_unit(k_to, row0_sm + 4 * i, pr.unit, zero);         // behind the last cached token
+                for (int i = 0; i < UNITS; ++i) store_unit(k_to, row0_sm + APART * i, pr.unit, zero);         // behind the last cached token
             fence_async_smem();
             mbar_arrive(smem_u32(&sh.k_full[stage]));
             if (next >= 0) pr.load_keys(p.pool, next);
@@ -555,7 +553,7 @@ __device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk 
             if (tok >= 0) pr.template store_values<BF>(v_to, row0_sm, vs_top, vz_top);
             else
 #pragma unroll
-                for (int i = 0; i < 8; ++i) store_unit(v_to, row0_sm + 4 * i, pr.unit, zero);
+                for (int i = 0; i < UNITS; ++i) store_unit(v_to, row0_sm + APART * i, pr.unit, zero);
             if (j == sg.n - 1) publish();
             fence_async_smem();
             mbar_arrive(smem_u32(&sh.v_full[stage]));
@@ -572,8 +570,8 @@ __device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk 
                 if (side == 0) wait_for(sh.k_empty[stage], parity, sh.failed, p.status);
                 else wait_for(sh.v_empty[stage], parity, sh.failed, p.status);
 #pragma unroll 2
-                for (int i = 0; i < 8; ++i) {
-                    const int u = u0 + 4 * i;
+                for (int i = 0; i < UNITS; ++i) {
+                    const int u = u0 + APART * i;
                     uint32_t x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8];
                     if (u < sg.most) {
                         const __nv_bfloat16 *from = src + (long long)(w.sq.k0 + u) * st + (long long)w.pl.h * shd + 16 * pr.unit;
@@ -597,7 +595,7 @@ __device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk 
                         atomicMax(&sh.odd_last, u);
                     }
                     unit_of_bf16<BITS>(x, BF, y);
-                    store_unit(side == 0 ? k_to : v_to, row0_sm + 4 * i, pr.unit, y);
+                    store_unit(side == 0 ? k_to : v_to, row0_sm + APART * i, pr.unit, y);
                 }
                 if (side == 1 && j == sg.n - 1) publish();
                 fence_async_smem();
@@ -611,10 +609,10 @@ template <int BITS, int G, bool M16, int TILES>
 __device__ __forceinline__ void producer_role(const ChunkParams &p, Walk w, Shared<TILES> &sh, unsigned char *k_sm, unsigned char *v_sm)
 {
     using S = Plan<TILES>;
-    const int pt = threadIdx.x - S::SOFT, group32 = pt / 32;
+    const int pt = threadIdx.x - S::SOFT, group32 = pt / 64;
     Producer<BITS, G, M16> pr;
-    pr.sub = pt / 8 % 4;
-    pr.unit = pt % 8;
+    pr.sub = (pt >> 2 & 1) | (pt >> 4 & 1) << 1 | (pt >> 5 & 1) << 2;
+    pr.unit = (pt & 3) | (pt >> 3 & 1) << 2;
     unsigned kv = 0;                                 // tiles so far
     Segment sg;
     while (walk_segment<S::ROWS>(p, w, sg)) {
@@ -709,7 +707,7 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
     __shared__ Shared<TILES> sh;
     unsigned char *q_sm = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024, *k_sm = q_sm + TILES * OPERAND, *v_sm = k_sm + S::STAGES * OPERAND;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-    constexpr int SOFT_WARPS = S::SOFT / 32, MMA_WARP = SOFT_WARPS + 4;
+    constexpr int SOFT_WARPS = S::SOFT / 32, MMA_WARP = SOFT_WARPS + S::PRODUCERS / 32;
     ChunkParams p = params;
     grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
     long long per, total;
@@ -727,8 +725,8 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
     }
     if (tid == 0) {
         for (int i = 0; i < S::STAGES; ++i) {
-            mbar_init(smem_u32(&sh.k_full[i]), 128);
-            mbar_init(smem_u32(&sh.v_full[i]), 128);
+            mbar_init(smem_u32(&sh.k_full[i]), S::PRODUCERS);
+            mbar_init(smem_u32(&sh.v_full[i]), S::PRODUCERS);
             mbar_init(smem_u32(&sh.k_empty[i]), 1);
             mbar_init(smem_u32(&sh.v_empty[i]), 1);
         }
@@ -749,7 +747,7 @@ __global__ void __launch_bounds__(Plan<TILES>::THREADS, Plan<TILES>::CTAS) chunk
         more_registers<S::SOFT_REGS>();
         softmax_role<BITS, TILES>(p, w, sh, q_sm, tmem);
     } else if (warp < MMA_WARP) {
-        more_registers<S::PRODUCER_REGS>();
+        if (S::PRODUCER_REGS < S::LAUNCH_REGS) fewer_registers<S::PRODUCER_REGS>();
         producer_role<BITS, G, M16, TILES>(p, w, sh, k_sm, v_sm);
     } else {
         fewer_registers<S::PRODUCT_REGS>();
