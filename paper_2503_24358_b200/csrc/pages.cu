@@ -441,12 +441,14 @@ __device__ __forceinline__ u64 codes_as_floats(unsigned word)
 }
 
 // grid (runs of tokens, heads, keys / values): a thread takes eight channels of eight consecutive tokens, which lie in one
-// group, so the eight scales and zero-points of a key group are read once for all of them; a half-warp's stores are whole rows
+// group, so the eight scales and zero-points of a key group are read once for all of them.  A half-warp's stores are whole rows: channels
+// 8 c .. of a bf16 row, 4 c .. and 64 + 4 c .. of a float32 row.
 template <int G, int BITS, bool BF16, bool M16>
 __global__ void __launch_bounds__(READ_THREADS, 4) pages_read_kernel(PagesParams p)
 {
-    constexpr int TOK = 8;
-    const int part = p.first + blockIdx.z, h = blockIdx.y, c8 = threadIdx.x & 15;
+    constexpr int TOK = 8, APART = BF16 ? 4 : D / 2;             // from the thread's first four channels to its others
+    constexpr int VG = !BF16 && G <= D / 2 ? 2 : 1;              // value groups of a token that its channels lie in
+    const int part = p.first + blockIdx.z, h = blockIdx.y, c8 = threadIdx.x & 15, c0 = c8 * (BF16 ? 8 : 4);
     const long long run = (long long)blockIdx.x * (READ_THREADS / 16) + (threadIdx.x >> 4);
     const int group = (int)(run / (G / TOK)), in_group = (int)(run % (G / TOK)) * TOK;
     const unsigned char *codes = part == 0 ? p.pool.kc : p.pool.vc;
@@ -457,48 +459,56 @@ __global__ void __launch_bounds__(READ_THREADS, 4) pages_read_kernel(PagesParams
     long long tok = group_token<G>(p, slots, group, h);
     if (tok < 0) return;
     tok += in_group;
-    unsigned words[TOK];
-    const unsigned char *from = codes + tok * (D * BITS / 8) + c8 * BITS;
+    unsigned words[TOK];                         // eight codes
+    const unsigned char *from = codes + tok * (D * BITS / 8) + c0 * BITS / 8;
 #pragma unroll
-    for (int i = 0; i < TOK; ++i)
-        words[i] = BITS == 2 ? (unsigned)__ldg(reinterpret_cast<const unsigned short *>(from + i * (D * BITS / 8))) : __ldg(reinterpret_cast<const unsigned *>(from + i * (D * BITS / 8)));
+    for (int i = 0; i < TOK; ++i) {
+        const unsigned char *f = from + i * (D * BITS / 8);
+        if (BF16) words[i] = BITS == 2 ? (unsigned)__ldg(reinterpret_cast<const unsigned short *>(f)) : __ldg(reinterpret_cast<const unsigned *>(f));
+        else if (BITS == 2) words[i] = (unsigned)__ldg(f) | (unsigned)__ldg(f + D / 2 * BITS / 8) << 8;
+        else words[i] = (unsigned)__ldg(reinterpret_cast<const unsigned short *>(f)) | (unsigned)__ldg(reinterpret_cast<const unsigned short *>(f + D / 2 * BITS / 8)) << 16;
+    }
     u64 s2[4], z2[4];                            // of the channels (keys)
-    float sv[TOK], zv[TOK];                      // of the tokens (values)
+    float sv[TOK][VG], zv[TOK][VG];              // of the tokens (values)
     if (part == 0) {
-        const long long at = tok / G * D + 8 * c8;
-        if (M16) {
-            const uint4 a = ldg128(static_cast<const __half *>(scales) + at), b = ldg128(static_cast<const __half *>(zeros) + at);
-            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+        const long long at = tok / G * D + c0;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const float2 u = __half22float2(*reinterpret_cast<const __half2 *>(&aw[c])), v = __half22float2(*reinterpret_cast<const __half2 *>(&bw[c]));
-                s2[c] = pack2(u.x, u.y);
-                z2[c] = pack2(v.x, v.y);
-            }
-        } else {
+        for (int c = 0; c < 2; ++c) {
+            if (M16) {
+                const uint2 a = __ldg(reinterpret_cast<const uint2 *>(static_cast<const __half *>(scales) + at + APART * c)), b = __ldg(reinterpret_cast<const uint2 *>(static_cast<const __half *>(zeros) + at + APART * c));
+                const uint32_t aw[2] = {a.x, a.y}, bw[2] = {b.x, b.y};
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const float4 u = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(scales) + at) + c), v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(zeros) + at) + c);
+                for (int k = 0; k < 2; ++k) {
+                    const float2 u = __half22float2(*reinterpret_cast<const __half2 *>(&aw[k])), v = __half22float2(*reinterpret_cast<const __half2 *>(&bw[k]));
+                    s2[2 * c + k] = pack2(u.x, u.y);
+                    z2[2 * c + k] = pack2(v.x, v.y);
+                }
+            } else {
+                const float4 u = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(scales) + at + APART * c)), v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(zeros) + at + APART * c));
                 s2[2 * c] = pack2(u.x, u.y); s2[2 * c + 1] = pack2(u.z, u.w);
                 z2[2 * c] = pack2(v.x, v.y); z2[2 * c + 1] = pack2(v.z, v.w);
             }
         }
     } else {
-        const long long at = tok * (D / G) + c8 / (G / 8);
+        const long long at = tok * (D / G) + c0 / G;
 #pragma unroll
-        for (int i = 0; i < TOK; ++i) {
-            sv[i] = load_meta<M16>(scales, at + i * (D / G));
-            zv[i] = load_meta<M16>(zeros, at + i * (D / G));
-        }
+        for (int i = 0; i < TOK; ++i)
+#pragma unroll
+            for (int k = 0; k < VG; ++k) {
+                sv[i][k] = load_meta<M16>(scales, at + i * (D / G) + APART / G * k);
+                zv[i][k] = load_meta<M16>(zeros, at + i * (D / G) + APART / G * k);
+            }
     }
-    const long long at = ((long long)group * G + in_group) * p.xt[part] + (long long)h * p.xh[part] + 8 * c8;
+    const long long at = ((long long)group * G + in_group) * p.xt[part] + (long long)h * p.xh[part] + c0;
 #pragma unroll
     for (int i = 0; i < TOK; ++i) {
         const u64 code2[4] = {codes_as_floats<BITS, 0>(words[i]), codes_as_floats<BITS, 1>(words[i]), codes_as_floats<BITS, 2>(words[i]), codes_as_floats<BITS, 3>(words[i])};
         float y[8];
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-            unpack2(part == 0 ? ffma2(code2[c], s2[c], z2[c]) : ffma2(code2[c], pack2(sv[i], sv[i]), pack2(zv[i], zv[i])), y[2 * c], y[2 * c + 1]);
+        for (int c = 0; c < 4; ++c) {
+            const float s = sv[i][c / 2 % VG], z = zv[i][c / 2 % VG];
+            unpack2(part == 0 ? ffma2(code2[c], s2[c], z2[c]) : ffma2(code2[c], pack2(s, s), pack2(z, z)), y[2 * c], y[2 * c + 1]);
+        }
         const long long to = at + i * p.xt[part];
         if (BF16) {
             uint32_t w[4];
@@ -509,9 +519,9 @@ __global__ void __launch_bounds__(READ_THREADS, 4) pages_read_kernel(PagesParams
             }
             *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y[part]) + to) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
-            float4 *f = reinterpret_cast<float4 *>(static_cast<float *>(p.y[part]) + to);
-            f[0] = make_float4(y[0], y[1], y[2], y[3]);
-            f[1] = make_float4(y[4], y[5], y[6], y[7]);
+            float *f = static_cast<float *>(p.y[part]) + to;
+            *reinterpret_cast<float4 *>(f) = make_float4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<float4 *>(f + APART) = make_float4(y[4], y[5], y[6], y[7]);
         }
     }
 }
