@@ -137,20 +137,33 @@ __device__ __forceinline__ void softmax_step(Acc<NT> &acc, float (&s)[NT][2][4],
     }
 }
 
-// Scales or zero-points of two neighbouring pairs: channels (lo, lo + HALF) and (lo + 1, lo + 1 + HALF) of the lane's 32.
+// The key metadata of a step in the operand's order, binary16, in the place of the first half of what was loaded: for a quarter of the channels
+// eight 16-byte pieces, scales of two neighbouring pairs (channels lo, lo + HALF and lo + 1, lo + 1 + HALF) and their zero-points.  A
+// lane makes one of them for the eight lanes that use it.
+constexpr int PAIRS_QUARTER = 8 * 16 + 16;           // padded: the four quarters fall on distinct banks
 template <int BITS, bool M16>
-__device__ __forceinline__ void meta_pairs(const unsigned char *from, int lo, __half2 (&y)[2])
+__device__ __forceinline__ void order_key_meta(unsigned char *st)
 {
+    using S = Stage<BITS, M16>;
     constexpr int HALF = BITS == 2 ? 8 : 4;          // codes in half a word; a pair is (c, c + HALF) of a word
-    if (M16) {
-        const uint32_t a = reinterpret_cast<const uint32_t *>(from)[lo / 2], b = reinterpret_cast<const uint32_t *>(from)[(lo + HALF) / 2];
-        y[0] = as_half2(pair16(a, b, 0));
-        y[1] = as_half2(pair16(a, b, 1));
-    } else {
-        const float2 a = reinterpret_cast<const float2 *>(from)[lo / 2], b = reinterpret_cast<const float2 *>(from)[(lo + HALF) / 2];
-        y[0] = __floats2half2_rn(a.x, b.x);
-        y[1] = __floats2half2_rn(a.y, b.y);
+    const int lane = threadIdx.x & 31, quarter = lane >> 3, m = 2 * (lane & 7), lo = m / HALF * 2 * HALF + m % HALF;
+    uint32_t y[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const unsigned char *from = st + (e ? S::KZ : S::KS) + quarter * S::QUARTER;
+        if (M16) {
+            const uint32_t a = reinterpret_cast<const uint32_t *>(from)[lo / 2], b = reinterpret_cast<const uint32_t *>(from)[(lo + HALF) / 2];
+            y[2 * e] = pair16(a, b, 0);
+            y[2 * e + 1] = pair16(a, b, 1);
+        } else {
+            const float2 a = reinterpret_cast<const float2 *>(from)[lo / 2], b = reinterpret_cast<const float2 *>(from)[(lo + HALF) / 2];
+            y[2 * e] = pack16<false>(a.x, b.x);
+            y[2 * e + 1] = pack16<false>(a.y, b.y);
+        }
     }
+    __syncwarp();
+    *reinterpret_cast<uint4 *>(st + S::KS + quarter * PAIRS_QUARTER + (lane & 7) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
+    __syncwarp();
 }
 template <bool M16>
 __device__ __forceinline__ float meta_at(const unsigned char *from, int i)
@@ -160,7 +173,7 @@ __device__ __forceinline__ float meta_at(const unsigned char *from, int i)
 
 // A step of cached tokens, staged at `st`.
 template <int BITS, bool M16, int NT, bool BF>
-__device__ __forceinline__ void cached_step(const unsigned char *st, const CodeBias<BITS> &bias, int g_shift, const Queries<NT> &queries, float scale_log2, Acc<NT> &acc, Range &range)
+__device__ __forceinline__ void cached_step(unsigned char *st, const CodeBias<BITS> &bias, int g_shift, const Queries<NT> &queries, float scale_log2, Acc<NT> &acc, Range &range)
 {
     using S = Stage<BITS, M16>;
     const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
@@ -172,6 +185,7 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, const CodeB
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[t][k][e] = 0.0f;
+    if (!BF) order_key_meta<BITS, M16>(st);
     // For few rows it is less to scale the queries than the codes (16 products a row of eight rather than 128 differences and multiply-adds)
     constexpr bool FOLD = !BF && NT <= 2;
     {
@@ -197,8 +211,9 @@ __device__ __forceinline__ void cached_step(const unsigned char *st, const CodeB
                     const int c = 4 * four + 2 * two, lo = wd * 2 * HALF + c;
                     __half2 s2[2], z2[2];
                     if (!BF) {
-                        meta_pairs<BITS, M16>(ks, lo, s2);
-                        meta_pairs<BITS, M16>(kz, lo, z2);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(st + S::KS + q * PAIRS_QUARTER + (wd * (HALF / 2) + 2 * four + two) * 16);
+                        s2[0] = as_half2(v.x); s2[1] = as_half2(v.y);
+                        z2[0] = as_half2(v.z); z2[1] = as_half2(v.w);
                     }
                     uint32_t b[NT][2];
 #pragma unroll
@@ -579,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, CTAS<NT>) chunk_rows_kernel(const __g
     __shared__ ChunkShared sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
     ChunkParams p = params;
-    grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
+    chunk_wait(p);
     long long per, total;
     chunk_share<R, STEP>(p, sh, per, total);
     const long long worker = (long long)blockIdx.x * WARPS + warp;
@@ -654,14 +669,16 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
 {
     __shared__ ChunkShared sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // The kernel for few rows lets this one begin when itself has waited for what came earlier, so lengths are there to be read; its
+    // parts are waited for below.
     ChunkParams p = params;
-    grid_wait(p.q, p.q_start, p.cached_len, p.page_table, p.new_start, p.new_len, p.k_new, p.v_new);
+    if (CTA_WORKERS) grid_wait(p.q_start, p.cached_len, p.new_start, p.new_len);
     long long per, total;
     chunk_share<ROWS, U>(p, sh, per, total);
     constexpr int WORKERS = CTA_WORKERS ? 1 : WARPS;
     const long long c0 = (long long)blockIdx.x * WORKERS, c = c0 + (CTA_WORKERS ? 0 : warp), border = (c + 1) * per;
-    if ((c0 + 1) * per >= total) return;
-    chunk_locate<ROWS, U, WORKERS>(p, sh, (c0 + 1) * per, per);
+    if ((c0 + 1) * per < total) chunk_locate<ROWS, U, WORKERS>(p, sh, (c0 + 1) * per, per);
+    if (!CTA_WORKERS) grid_wait(p.part, p.ml);
     if (border >= total) return;
     const ChunkPlace pl = sh.found[CTA_WORKERS ? 0 : warp];
     const long long first = border - pl.at + p.start;        // place of the item's first tile

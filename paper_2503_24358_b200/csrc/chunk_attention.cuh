@@ -82,12 +82,23 @@ struct ChunkShared {
     ChunkPlace found[4];
 };
 
+// As grid_wait, but the kernel behind (the sum of the parts) may begin only now: it reads the lengths before it waits itself.
+__device__ __forceinline__ void chunk_wait(ChunkParams &p)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("" : "+l"(p.q), "+l"(p.q_start), "+l"(p.cached_len), "+l"(p.page_table), "+l"(p.new_start), "+l"(p.new_len), "+l"(p.k_new), "+l"(p.v_new)::"memory");
+}
+
 // All threads of the CTA (a multiple of 32, at most 1024) call this.  per: places per worker, total: of all sequences.
 template <int R, int U>
 __device__ __forceinline__ void chunk_share(const ChunkParams &p, ChunkShared &sm, long long &per, long long &total)
 {
     long long mine = 0;
-    for (int i = threadIdx.x; i < p.n_seqs; i += blockDim.x) mine += chunk_head_tiles<R, U>(p, chunk_seq(p, i)) * p.H;
+    for (int i = threadIdx.x; i < p.n_seqs; i += blockDim.x) {
+        const ChunkSeq s = chunk_seq(p, i);
+        mine += chunk_head_tiles<R, U>(p, s) * p.H;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     if ((threadIdx.x & 31) == 0) sm.sums[threadIdx.x >> 5] = mine;
