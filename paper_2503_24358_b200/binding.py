@@ -610,6 +610,12 @@ class RopePlan:
 _NO_ROWS = (None, 0, 0, 0, None, 0, 0)
 
 
+def _on_current_device(x, name):
+    """Kernels run on the current device, with its stream; memory of another one they could not reach."""
+    if x.is_cuda and x.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {x.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
 def _rows(x, name):
     """Address and strides of [tokens, heads, d]."""
     strides = x.stride()
@@ -632,6 +638,7 @@ def squat_rope_apply(plan: RopePlan, positions: torch.Tensor, q: torch.Tensor = 
     x = q if q is not None else k
     if x is None:
         return
+    _on_current_device(x, "q")
     dtype = x.dtype
     T, _, d = x.shape
     if positions.shape != (plan.n_axes, T) or (T > 1 and positions.stride(1) != 1):
@@ -716,6 +723,7 @@ def _int32(t, name, numel):
 
 def _pool_rows(pool, slots, tensors, names):
     """Token count and dtype of the key and value rows that come with `slots`, and their addresses and strides."""
+    _on_current_device(slots, "slots")
     T = slots.numel() * pool.group_size
     want = (T, pool.n_kv_heads, pool.head_dim)
     args, dtype = [], None
@@ -774,6 +782,7 @@ def squat_chunk_attention(q: torch.Tensor, pool: PagePool, q_start: torch.Tensor
     k_new / v_new[new_start[i]:][:new_len[i]] (bfloat16 [rows, n_kv_heads, d]).  Index tensors are int32 on the device and are
     read there; max_q is the largest number of queries of a sequence.  workspace: CUDA uint8 of
     squat_chunk_attention_workspace_bytes(n_q, n_q_heads, n_kv_heads, max_q)."""
+    _on_current_device(q, "q")
     n_seqs, bf16, shape, d = cached_len.numel(), torch.bfloat16, q.shape, pool.head_dim
     if len(shape) != 3 or shape != out.shape or q.dtype is not bf16 or out.dtype is not bf16 or shape[2] != d:
         raise ValueError("q and out must be bfloat16 [n_q, n_q_heads, head_dim]")

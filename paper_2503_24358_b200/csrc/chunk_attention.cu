@@ -5,7 +5,7 @@
 //
 // The cache's bytes bound it, if the two instructions that a code costs can be issued meanwhile.  So nothing is staged for
 // the tensor core: the operands of mma.sync m16n8k16 are made in the registers where it wants them, the dequantized ones once for
-// up to 32 rows, 8 rows a product (the tcgen05 form wants them in shared or tensor memory, and 128 rows to fill it).
+// up to 24 rows, 8 rows a product (the tcgen05 form wants them in shared or tensor memory, and 128 rows to fill it).
 //   - A warp works by itself: it takes 32 tokens at a time (they lie in one page and one group of keys) of its own share of the work.
 //     (Warps that shared an item waited for one another at its end: a quarter of all stalls.)
 //   - Scores, transposed: tokens are the 16 side.  Lane (g, q) holds tokens g and g + 8, channels 32 q .. 32 q + 31: a contiguous
@@ -662,44 +662,44 @@ __global__ void __launch_bounds__(THREADS, CTAS<NT>) chunk_rows_kernel(const __g
     }
 }
 
-// The item that worker c began and did not finish, if there is one.  A warp takes a row at a time, four channels a lane; workers that
-// are CTAs have a CTA (and blockIdx.y) of warps here, workers that are warps a warp.
-template <int ROWS, int U, bool CTA_WORKERS>
+// The item that worker c = blockIdx.x began and did not finish, if there is one.  A warp takes a row, four channels a lane: all the
+// row's parts where they are few (BY_ROWS: parts of CTAs' work, of many rows), else every fourth, eight at once, which are joined.
+template <int ROWS, int U, bool BY_ROWS>
 __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant__ ChunkParams params)
 {
     __shared__ ChunkShared sh;
+    __shared__ float4 o_sm[BY_ROWS ? 1 : 4][32];
+    __shared__ float2 ml_sm[4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // The kernel for few rows lets this one begin when itself has waited for what came earlier, so lengths are there to be read; its
     // parts are waited for below.
     ChunkParams p = params;
-    if (CTA_WORKERS) grid_wait(p.q_start, p.cached_len, p.new_start, p.new_len);
+    if (BY_ROWS) grid_wait(p.q_start, p.cached_len, p.new_start, p.new_len);
     long long per, total;
     chunk_share<ROWS, U>(p, sh, per, total);
-    constexpr int WORKERS = CTA_WORKERS ? 1 : WARPS;
-    const long long c0 = (long long)blockIdx.x * WORKERS, c = c0 + (CTA_WORKERS ? 0 : warp), border = (c + 1) * per;
-    if ((c0 + 1) * per < total) chunk_locate<ROWS, U, WORKERS>(p, sh, (c0 + 1) * per, per);
-    if (!CTA_WORKERS) grid_wait(p.part, p.ml);
+    const long long c = blockIdx.x, border = (c + 1) * per;
+    if (border < total) chunk_locate<ROWS, U, 1>(p, sh, border, per);
+    if (!BY_ROWS) grid_wait(p.part, p.ml);
     if (border >= total) return;
-    const ChunkPlace pl = sh.found[CTA_WORKERS ? 0 : warp];
+    const ChunkPlace pl = sh.found[0];
     const long long first = border - pl.at + p.start;        // place of the item's first tile
     if (first >= border || first < c * per) return;
     const ChunkSeq sq = chunk_seq(p, pl.seq);
     const long long parts = (first + chunk_tiles<ROWS, U>(p, sq, pl.qt) - 1) / per - c + 1;
     const int row0 = pl.qt * ROWS, n_rows = min(ROWS, sq.nq * p.qpk - row0);
-    const int r_first = CTA_WORKERS ? blockIdx.y * 4 + warp : blockIdx.y, r_step = gridDim.y * (CTA_WORKERS ? 4 : 1);
+    constexpr int STRIDE = BY_ROWS ? 1 : 4, AT_ONCE = 8;     // parts of a warp: every STRIDE-th, so many in flight together
 #pragma unroll 1
-    for (int r = r_first; r < n_rows; r += r_step) {
+    for (int r = BY_ROWS ? blockIdx.y * 4 + warp : blockIdx.y; r < n_rows; r += gridDim.y * (BY_ROWS ? 4 : 1)) {
         float m = -INFINITY, l = 0.0f;
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        constexpr int AT_ONCE = 8;                   // parts whose loads are in flight together
 #pragma unroll 1
-        for (long long i0 = 0; i0 < parts; i0 += AT_ONCE) {
+        for (long long i0 = BY_ROWS ? 0 : warp; i0 < parts; i0 += AT_ONCE * STRIDE) {
             float2 v[AT_ONCE];
             float4 x[AT_ONCE];
 #pragma unroll
             for (int i = 0; i < AT_ONCE; ++i) {
-                const bool in = i0 + i < parts;
-                const long long at = ((i0 + i == 0 ? 2 * c + 1 : 2 * (c + i0 + i)) * ROWS + r);
+                const long long part = i0 + STRIDE * i, at = ((part == 0 ? 2 * c + 1 : 2 * (c + part)) * ROWS + r);
+                const bool in = part < parts;
                 v[i] = in ? *reinterpret_cast<const float2 *>(p.ml + at * 2) : make_float2(-INFINITY, 0.0f);
                 x[i] = in ? *reinterpret_cast<const float4 *>(p.part + at * D + 4 * lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
@@ -714,6 +714,27 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
                 const float f = exp2_fast(v[i].x - use);
                 l = fmaf(f, v[i].y, l);
                 o.x = fmaf(f, x[i].x, o.x); o.y = fmaf(f, x[i].y, o.y); o.z = fmaf(f, x[i].z, o.z); o.w = fmaf(f, x[i].w, o.w);
+            }
+            m = mn;
+        }
+        if (!BY_ROWS) {
+            __syncthreads();                         // (the row before this one has been read)
+            o_sm[warp][lane] = o;
+            if (lane == 0) ml_sm[warp] = make_float2(m, l);
+            __syncthreads();
+            if (warp != 0) continue;
+            float mn = m;
+#pragma unroll
+            for (int w = 1; w < 4; ++w) mn = max_nan(mn, ml_sm[w].x);
+            const float use = mn == -INFINITY ? 0.0f : mn, f0 = exp2_fast(m - use);
+            l *= f0;
+            o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+            for (int w = 1; w < 4; ++w) {
+                const float f = exp2_fast(ml_sm[w].x - use);
+                const float4 x = o_sm[w][lane];
+                l = fmaf(f, ml_sm[w].y, l);
+                o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
             }
             m = mn;
         }
@@ -741,24 +762,27 @@ int launch_rows_tiles(const ChunkParams &p, int bits, int meta16, cudaStream_t s
     return meta16 ? launch_rows<4, true, NT>(p, st) : launch_rows<4, false, NT>(p, st);
 }
 
-// The kernels of a call.  Sequences with at most few_rows rows per KV head go to the kernel for few rows (8 `eights` of them share an
-// item), the others to the kernel for many, in tiles of 128 or 256.
+// The kernels of a call.  Sequences with at most FEW_ROWS rows per KV head go to the kernel for few rows (8 `eights` of them share an
+// item), the others to the kernel for many, in tiles of 128 or 256.  Both sides, us a call, 32 / 8 heads, 2 bits: 16 sequences of up to 8160
+// tokens, 16 rows 84 and 119, 24 rows 81 and 120, 32 rows (in a kernel for four times eight) 105 and 114, 48 rows 163 and 138; two
+// such sequences, 24 rows 53 and 47, 32 rows 69 and 46; 32 of 2048 tokens at 4 bits, 24 rows 69 and 86, 32 rows 89 and 83.
 struct ChunkKernels {
     int eights;                                      // 0: no kernel for few rows
     int tiles;                                       // 0: no kernel for many rows
 };
-constexpr int FEW_ROWS = 32;
+constexpr int FEW_ROWS = 24;
 
 ChunkKernels kernels_for(long long n_q, long long n_seqs, long long max_q, int qpk)
 {
     ChunkKernels k;
     const long long most = max_q * qpk, rows = most <= FEW_ROWS ? most : qpk;
     k.tiles = most <= FEW_ROWS ? 0 : most <= 128 ? 1 : 2;
-    k.eights = rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
-    if (k.tiles && n_q == n_seqs * max_q) k.eights = 0;      // sequences of one length, all of them in the other kernel
+    k.eights = rows <= 8 ? 1 : rows <= 16 ? 2 : 3;
+    // sequences of one length, all of them in the other kernel; or heads that share keys in such numbers that one query is many rows
+    if (k.tiles && (n_q == n_seqs * max_q || qpk > FEW_ROWS)) k.eights = 0;
     return k;
 }
-int rows_workers(int eights) { return WARPS * squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : eights == 3 ? CTAS<3> : CTAS<4>); }
+int rows_workers(int eights) { return WARPS * squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : CTAS<3>); }
 int matrix_workers(int tiles) { return squat_sm_count() * (tiles == 2 ? 1 : 2); }
 size_t part_floats(int workers, int rows) { return 2 * (size_t)workers * rows * (D + 2); }
 // Workers, at most as many as the longest sequences that the page table can hold would give work to, and their parts.
@@ -774,7 +798,8 @@ template <int ROWS>
 int launch_combine(const ChunkParams &p, cudaStream_t st)
 {
     if (ROWS >= 128) return squat_launch(chunk_combine_kernel<ROWS, 128, true>, dim3((unsigned)p.n_workers, ROWS / 16), D, 0, st, p);
-    return squat_launch(chunk_combine_kernel<ROWS, STEP, false>, dim3((unsigned)(p.n_workers / WARPS), ROWS / 4), D, 0, st, p);
+    // (a CTA for every row that a decode step has; more rows than that in turns of four)
+    return squat_launch(chunk_combine_kernel<ROWS, STEP, false>, dim3((unsigned)p.n_workers, (unsigned)(p.qpk < ROWS / 4 ? p.qpk : ROWS / 4)), D, 0, st, p);
 }
 
 }  // namespace
@@ -815,12 +840,11 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
         switch (k.eights) {
             case 1: rc = launch_rows_tiles<1>(few, pool->bits, pool->meta16, st); break;
             case 2: rc = launch_rows_tiles<2>(few, pool->bits, pool->meta16, st); break;
-            case 3: rc = launch_rows_tiles<3>(few, pool->bits, pool->meta16, st); break;
-            default: rc = launch_rows_tiles<4>(few, pool->bits, pool->meta16, st); break;
+            default: rc = launch_rows_tiles<3>(few, pool->bits, pool->meta16, st); break;
         }
     }
     if (rc == SQUAT_OK && k.tiles) rc = k.tiles == 1 ? launch_combine<128>(many, st) : launch_combine<256>(many, st);
     if (rc == SQUAT_OK && k.eights)
-        rc = k.eights == 1 ? launch_combine<8>(few, st) : k.eights == 2 ? launch_combine<16>(few, st) : k.eights == 3 ? launch_combine<24>(few, st) : launch_combine<32>(few, st);
+        rc = k.eights == 1 ? launch_combine<8>(few, st) : k.eights == 2 ? launch_combine<16>(few, st) : launch_combine<24>(few, st);
     return rc;
 }
