@@ -49,8 +49,9 @@ typedef enum { SQUAT_KEYS = 0, SQUAT_VALUES = 1 } squat_kind;
 #define SQUAT_FLAG_NO_CONVERGE 4u   /* eigensolver hit its sweep limit for some head               */
 #define SQUAT_FLAG_BOUNDS 16u        /* only in the bounds-checked build of the library (-DSQUAT_CHECKED): a kernel computed an
                                        * address outside the buffer or on-chip region it belongs to; the access was skipped      */
-#define SQUAT_FLAG_DEVICE_TIMEOUT 8u /* a bounded wait on the tensor core inside squat_quantize_keys ran
-                                       * out: that call's outputs are invalid (the kernel still ends)  */
+#define SQUAT_FLAG_DEVICE_TIMEOUT 8u /* a bounded wait on the tensor core inside squat_quantize_keys or
+                                       * squat_chunk_attention ran out: that call's outputs are invalid
+                                       * (the kernel still ends)                                        */
 #define SQUAT_FLAG_PAGES 32u          /* a slot, page number, length or row range that a paged call read on the device lies
                                        * outside its limits: what it names was neither read nor written */
 
@@ -462,7 +463,7 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
  *                sequence's length are not used.
  *   k_new, v_new [n_new, n_kv_heads, d] bf16, d contiguous, element strides (multiples of 8 elements); sequence i's rows begin at
  *                new_start[i] (device int32), new_len[i] of them (device int32).  n_new = 0: all four may be NULL.
- *   max_q        the largest n_i, a host value that chooses the kernel; results are right for other values too.
+ *   max_q        the largest n_i, a host value that chooses the kernels; results are right for other values too.
  *   softmax_scale  0: 1 / sqrt(d).
  *   lse          NULL, or float32 [n_q, n_q_heads]: natural logarithm of the softmax's denominator.
  *   workspace    device, 256-byte aligned, at least squat_chunk_attention_workspace_bytes(...); nothing is kept in it between

@@ -288,3 +288,28 @@ def test_a_step_end_to_end():
             sq.squat_pages_write(pool, slots, k[take], v[take], s, wws)
         cached = [c + f for c, f in zip(cached, full)]
     assert cached == [96, 96]
+
+
+@pytest.mark.parametrize("heads, nq", [((8, 1), 1), ((9, 1), 1), ((8, 1), 2), ((17, 1), 1), ((8, 1), 3), ((5, 1), 5), ((24, 1), 1), ((25, 1), 1), ((8, 1), 16), ((43, 1), 3), ((16, 2), 32), ((1, 1), 257)])
+def test_row_counts_around_the_kernels_borders(heads, nq):
+    """8, 9, 16, 17, 24, 25, 128, 129, 256 and 257 rows per KV head, alone (sequences of one length) and with shorter sequences."""
+    for seqs in ([(nq, 416, nq), (nq, 32, nq + 3)], [(nq, 416, nq), (max(1, nq // 3), 704, 2), (1, 96, 1)]):
+        b = Batch(nq + heads[0], seqs, *heads, 2, 32, pages_of=3)
+        check(b, *call(b))
+
+
+def test_calls_at_the_same_time():
+    """Two streams, each with its workspace: few rows on one, many on the other."""
+    small = Batch(41, [(1, 1024, 9)] * 12, 8, 8, 2, 32)
+    large = Batch(43, [(90, 640, 97), (1, 320, 1), (200, 0, 200)], 8, 2, 4, 64, "f16")
+    want = [call(b, lse=False)[0] for b in (small, large)]
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.zeros_like(b.q) for b in (small, large)]
+    spaces = [torch.empty(sq.squat_chunk_attention_workspace_bytes(b.n_q, b.Hq, b.H, b.max_q), dtype=torch.uint8, device="cuda") for b in (small, large)]
+    pools = [sq.PagePool(*b.tensors) for b in (small, large)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, st, out, ws, pool in zip((small, large), streams, outs, spaces, pools):
+            sq.squat_chunk_attention(b.q, pool, b.q_start, b.cached, b.page_table, out, ws, b.max_q, b.k_new, b.v_new, b.new_start, b.new_len, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
