@@ -404,7 +404,7 @@ int squat_rope_apply(const squat_rope_plan *plan, const void *positions, int pos
 /*
  * A paged cache.  A page holds page_tokens tokens of every KV head in the layout of the cache above: token t of page p and
  * head h sits at token index p * page_stride + h * head_stride + t (strides in tokens, multiples of group_size; dense pages:
- * page_stride = n_kv_heads * page_tokens, head_stride = page_tokens).  A token index moves a code pointer by d * bits / 8 bytes, key
+ * page_stride = n_kv_heads * page_tokens, head_stride = page_tokens; pages that overlap are refused).  A token index moves a code pointer by d * bits / 8 bytes, key
  * metadata by d elements for every group_size tokens and value metadata by d / group_size elements.  page_tokens is a multiple of
  * group_size; the pool has fewer than 2^31 slots.  meta16 = 1: scales and zero-points are binary16.  The struct is read on the host
  * during a call; the memory is the caller's.  A sequence's tokens go to any pages in any order; slot p * page_tokens + t names a
@@ -441,7 +441,8 @@ int squat_pages_write(const squat_subspace *s, const squat_page_pool *pool, cons
 /*
  * Reads groups of tokens back from pages (squat_dequantize with places): row i * group_size + t of k_out and v_out
  * [n_tokens, n_kv_heads, d] becomes the token at slots[i] + t.  Rows of a negative slot are left as they were, and so are those of a
- * slot outside the pool (SQUAT_FLAG_PAGES).  Either output may be NULL.  Element strides are multiples of 16 bytes.
+ * slot outside the pool (SQUAT_FLAG_PAGES).  Either output may be NULL.  Element strides are multiples of 16 bytes; rows that
+ * overlap are refused.
  */
 int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens, int out_dtype,
                      void *k_out, long long k_stride_t, long long k_stride_h,
@@ -460,7 +461,7 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
  *                they were.
  *   cached_len   device int32 [n_seqs], multiples of group_size, at most table_stride * page_tokens.
  *   page_table   device int32 [n_seqs, table_stride]: page j holds the sequence's tokens j * page_tokens on.  Entries past a
- *                sequence's length are not used.
+ *                sequence's length are not used.  table_stride * page_tokens and n_new are at most 2^31 - 256.
  *   k_new, v_new [n_new, n_kv_heads, d] bf16, d contiguous, element strides (multiples of 8 elements); sequence i's rows begin at
  *                new_start[i] (device int32), new_len[i] of them (device int32).  n_new = 0: all four may be NULL.
  *   max_q        the largest n_i, a host value that chooses the kernels; results are right for other values too.

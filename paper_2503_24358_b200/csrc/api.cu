@@ -651,6 +651,16 @@ int squat_rope_plan_fill(double base, int head_dim, const int *sections, int n_a
     return SQUAT_OK;
 }
 
+namespace {
+// Whether n x m blocks of `size` elements lie apart: those of one dimension within a step of the other
+bool lie_apart(long long n, long long stride_n, long long m, long long stride_m, long long size)
+{
+    if (n <= 0 || m <= 0) return true;
+    const __int128 span_n = (__int128)(n - 1) * stride_n + size, span_m = (__int128)(m - 1) * stride_m + size;
+    return (n == 1 || stride_n >= size) && (m == 1 || stride_m >= size) && (n == 1 || m == 1 || stride_n >= span_m || stride_m >= span_n);
+}
+}  // namespace
+
 int squat_rope_apply(const squat_rope_plan *plan, const void *positions, int positions64, long long axis_stride, int n_tokens,
                      int head_dim, int dtype, int inverse,
                      const void *q, int n_q_heads, long long q_stride_t, long long q_stride_h,
@@ -670,6 +680,7 @@ int squat_rope_apply(const squat_rope_plan *plan, const void *positions, int pos
     const int heads[2] = {n_q_heads, n_k_heads};
     const long long strides[2][4] = {{q_stride_t, q_stride_h, q_out_stride_t, q_out_stride_h}, {k_stride_t, k_stride_h, k_out_stride_t, k_out_stride_h}};
     const long long vec = 16 / (long long)elem_size(dtype);
+    if ((long long)n_q_heads + n_k_heads > 0x7fffffffLL) return SQUAT_ERR_UNSUPPORTED;
     if (n_tokens == 0 || n_q_heads + n_k_heads == 0) return SQUAT_OK;
     if (!positions || (reinterpret_cast<uintptr_t>(positions) & (positions64 ? 7u : 3u))) return SQUAT_ERR_INVALID_ARG;
     for (int i = 0; i < 2; ++i) {
@@ -678,7 +689,7 @@ int squat_rope_apply(const squat_rope_plan *plan, const void *positions, int pos
         for (int j = 0; j < 4; ++j)
             if (strides[i][j] < 0 || strides[i][j] % vec) return SQUAT_ERR_INVALID_ARG;
         // no two output rows in one place, and rows that are written in place stay where they are read
-        if ((n_tokens > 1 && strides[i][2] < D) || (heads[i] > 1 && strides[i][3] < D)) return SQUAT_ERR_INVALID_ARG;
+        if (!lie_apart(n_tokens, strides[i][2], heads[i], strides[i][3], D)) return SQUAT_ERR_INVALID_ARG;
         if (x[i] == y[i] && ((n_tokens > 1 && strides[i][0] != strides[i][2]) || (heads[i] > 1 && strides[i][1] != strides[i][3]))) return SQUAT_ERR_INVALID_ARG;
     }
     return squat_launch_rope(plan, positions, positions64, axis_stride, n_tokens, dtype, inverse, x, y, heads, strides, static_cast<cudaStream_t>(stream));
@@ -694,7 +705,7 @@ int check_pool(const squat_page_pool *p)
     if (p->group_size != 32 && p->group_size != 64 && p->group_size != 128) return SQUAT_ERR_UNSUPPORTED;
     if (p->page_tokens % p->group_size || p->page_stride % p->group_size || p->head_stride % p->group_size) return SQUAT_ERR_SHAPE;
     if ((long long)p->n_pages * p->page_tokens > 0x7fffffffLL || p->n_kv_heads > 65535) return SQUAT_ERR_UNSUPPORTED;      // a slot is an int
-    if ((p->n_kv_heads > 1 && p->head_stride < p->page_tokens) || (p->n_pages > 1 && p->page_stride < p->page_tokens)) return SQUAT_ERR_INVALID_ARG;
+    if (!lie_apart(p->n_pages, p->page_stride, p->n_kv_heads, p->head_stride, p->page_tokens)) return SQUAT_ERR_INVALID_ARG;
     if (p->n_pages > 0 && (!p->k_codes || !p->k_scales || !p->k_zeros || !p->v_codes || !p->v_scales || !p->v_zeros)) return SQUAT_ERR_INVALID_ARG;
     if (!aligned16(p->k_codes) || !aligned16(p->k_scales) || !aligned16(p->k_zeros) || !aligned16(p->v_codes) || !aligned16(p->v_scales) || !aligned16(p->v_zeros))
         return SQUAT_ERR_INVALID_ARG;
@@ -707,7 +718,7 @@ int check_rows(const void *x, long long stride_t, long long stride_h, int n_toke
 {
     const long long vec = 16 / (long long)elem_size(dtype);
     if (!aligned16(x) || stride_t < 0 || stride_h < 0 || stride_t % vec || stride_h % vec) return SQUAT_ERR_INVALID_ARG;
-    if (written && ((n_tokens > 1 && stride_t < D) || (heads > 1 && stride_h < D))) return SQUAT_ERR_INVALID_ARG;
+    if (written && !lie_apart(n_tokens, stride_t, heads, stride_h, D)) return SQUAT_ERR_INVALID_ARG;
     return SQUAT_OK;
 }
 
@@ -808,6 +819,8 @@ int squat_chunk_attention(const void *q, int n_q, int n_q_heads, long long q_str
     if (!(softmax_scale >= 0.0f) || !std::isfinite(softmax_scale)) return SQUAT_ERR_INVALID_ARG;
     if (n_q_heads % pool->n_kv_heads) return SQUAT_ERR_SHAPE;
     if ((long long)n_q * n_q_heads > 0x7fffffffLL) return SQUAT_ERR_UNSUPPORTED;
+    // (a sequence's tokens are counted in 32 bits, rounded up to tiles of up to 256)
+    if (n_new > 0x7fffff00 || (long long)table_stride * pool->page_tokens > 0x7fffff00LL) return SQUAT_ERR_UNSUPPORTED;
     if ((rc = check_rows(q, q_stride_t, q_stride_h, n_q, n_q_heads, SQUAT_BF16, false)) != SQUAT_OK) return rc;
     if ((rc = check_rows(out, out_stride_t, out_stride_h, n_q, n_q_heads, SQUAT_BF16, true)) != SQUAT_OK) return rc;
     if (n_q == 0 || n_seqs == 0) return SQUAT_OK;

