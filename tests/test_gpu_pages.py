@@ -217,3 +217,40 @@ def test_graph_replay_with_other_places():
     ref = torch.empty_like(k), torch.empty_like(v)
     sq.squat_pages_read(pool, torch.tensor([0, 32], dtype=torch.int32, device="cuda"), *ref)
     assert torch.equal(out[0], ref[0]) and torch.equal(out[1], ref[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_error_feedback_from_a_shared_projection_in_a_graph(dtype):
+    H, G, bits, groups = 2, 32, 2, 6
+    g = gen(11)
+    projection = normal(g, groups * G, 4 * H, D).to(dtype)     # queries of two heads each, keys, values
+    k, v = projection[:, 2 * H:3 * H], projection[:, 3 * H:]
+    s = sq.Subspace(H)
+    sq.squat_build_subspace(s, normal(g, 2 * H, 300, D).to(torch.bfloat16), 8, 1e-3, 1)
+    pool = sq.PagePool.empty(5, 64, H, bits, G)
+    blank = [t.zero_() for t in pool.tensors]
+    slots = torch.tensor([64, -1, 0, 288, 128, 32], dtype=torch.int32, device="cuda")
+    ws = torch.empty(sq.squat_pages_write_workspace_bytes(pool, groups * G), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        sq.squat_pages_write(pool, slots, k, v, s, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sq.squat_pages_write(pool, slots, k, v, s, ws)
+    for t in blank:
+        t.zero_()
+    projection.copy_(normal(g, groups * G, 4 * H, D).to(dtype))
+    slots.copy_(torch.tensor([256, 32, -1, 96, 160, 0], dtype=torch.int32))
+    graph.replay()
+    torch.cuda.synchronize()
+    written = [0, 1, 3, 4, 5]
+    got = at_slots(pool.tensors, slots[written], 64, G)
+    rows = torch.tensor(written, device="cuda").repeat_interleave(G) * G + torch.arange(G, device="cuda").repeat(len(written))
+    want = contiguous(s, k[rows].contiguous(), v[rows].contiguous(), bits, G, "f32")
+    for i in (0, 1, 2, 5):                                    # keys, and the values' zero-points
+        assert torch.equal(got[i], want[i])
+    free = torch.ones(5, 2, dtype=torch.bool, device="cuda")
+    free[slots[written].long() // 64, slots[written].long() % 64 // G] = False
+    assert not any(pool.tensors[i].unflatten(2, (2, -1)).transpose(1, 2)[free].any() for i in (0, 3))
