@@ -143,6 +143,11 @@ struct Row8<true> {
         const uint32_t w = i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w;
         return pack2(bf16lo_to_f32(w), bf16hi_to_f32(w));
     }
+    __device__ __forceinline__ void blank(int i, bool lo, bool hi)            // channels of pair i become zero
+    {
+        uint32_t &w = i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w;
+        w &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    }
 };
 template <>
 struct Row8<false> {
@@ -154,6 +159,13 @@ struct Row8<false> {
         b = __ldg(s + 1);
     }
     __device__ __forceinline__ u64 pair(int i) const { return i == 0 ? pack2(a.x, a.y) : i == 1 ? pack2(a.z, a.w) : i == 2 ? pack2(b.x, b.y) : pack2(b.z, b.w); }
+    __device__ __forceinline__ void blank(int i, bool lo, bool hi)
+    {
+        float4 &v = i < 2 ? a : b;
+        float &x = i % 2 ? v.z : v.x, &y = i % 2 ? v.w : v.y;
+        x = lo ? 0.0f : x;
+        y = hi ? 0.0f : y;
+    }
 };
 // Minimum and maximum of pairs of channels: packed bf16, or two floats.
 template <bool BF16>
@@ -291,6 +303,17 @@ __device__ __forceinline__ void write_keys(const PagesParams &p, const void *src
         rb2[c] = pack2(a.rb, b.rb);
         keep |= (a.ok ? ((1u << BITS) - 1u) << (BITS * 2 * c) : 0u) | (b.ok ? ((1u << BITS) - 1u) << (BITS * (2 * c + 1)) : 0u);
         slow |= (a.fast ? 0u : 1u << (BITS * 2 * c)) | (b.fast ? 0u : 1u << (BITS * (2 * c + 1)));
+        // Channels without a grid, or with one beyond the bracket's range: their ends are no codes (0 times infinity, as a rule), and in the
+        // sum of a word they would spill into the fields above.  They enter it as zeros; those with a grid are decided by the division
+        // below.  (Ends that are clamped spill nothing.)
+        if (!M16 && !(a.ok && a.fast && b.ok && b.fast)) {
+            const bool lo = !(a.ok && a.fast), hi = !(b.ok && b.fast);
+            zero2[c] = pack2(lo ? 0.0f : z.x, hi ? 0.0f : z.y);
+            ra2[c] = pack2(lo ? 0.0f : a.ra, hi ? 0.0f : b.ra);
+            rb2[c] = pack2(lo ? 0.0f : a.rb, hi ? 0.0f : b.rb);
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) x[i].blank(c, lo, hi);
+        }
     }
     // words first; the open ones of all rows then in one loop, so that a warp's lanes take theirs at the same time
     unsigned rows = 0;

@@ -1,5 +1,7 @@
 """GPU: groups quantized into pages and read back, bit by bit against the definition; keys with error feedback against the
 quantizer of contiguous caches, whose bytes they are, and what is read back against its dequantizer."""
+import math
+
 import pytest
 import torch
 
@@ -254,3 +256,62 @@ def test_error_feedback_from_a_shared_projection_in_a_graph(dtype):
     free = torch.ones(5, 2, dtype=torch.bool, device="cuda")
     free[slots[written].long() // 64, slots[written].long() % 64 // G] = False
     assert not any(pool.tensors[i].unflatten(2, (2, -1)).transpose(1, 2)[free].any() for i in (0, 3))
+
+
+def odd_group(x, kind):
+    """A group [n] whose grid is no ordinary one."""
+    y = x.clone()
+    if kind == "constant":
+        y[:] = 1.5
+    elif kind == "zero":
+        y[:] = 0.0
+    elif kind in ("nan", "inf", "-inf"):
+        y[len(y) // 3] = float(kind)
+    elif kind == "infinite range":
+        y[0], y[1] = 3e38, -3e38
+    else:
+        y *= {"subnormal scale": 3e-39, "tiny scale": 1e-32, "huge scale": 1e33}[kind]
+    return y
+
+
+KINDS = ["constant", "zero", "nan", "inf", "-inf", "infinite range", "subnormal scale", "tiny scale", "huge scale"]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("meta", ["f32", "f16"])
+@pytest.mark.parametrize("bits, G", [(2, 32), (4, 32), (2, 64), (4, 128)])
+def test_odd_groups_leave_their_neighbours_alone(kind, dtype, meta, bits, G):
+    """Codes, grids and flags of groups with a constant or not finite channel (token), or one whose scale is far from 1: every
+    code by the definition, in float64 (values in float32) on the stored grid, of the odd groups and of those beside them."""
+    H, L = 2, 2 ** bits - 1
+    k, v, _ = inputs(bits + G, G, H, torch.float32)
+    for j in range(8):                                        # one at every place of an octet, then two, then all eight
+        k[:, 0, 8 * j + j] = odd_group(k[:, 0, 8 * j + j], kind)
+        for c in (8 * (8 + j) + j, 8 * (8 + j) + (j + 3) % 8):
+            k[:, 0, c] = odd_group(k[:, 0, c], kind)
+    for c in range(40, 48):
+        k[:, 1, c] = odd_group(k[:, 1, c], kind)
+    for t in range(0, G, 3):
+        a = t // 3 % (D // G) * G
+        v[t, t % H, a:a + G] = odd_group(v[t, t % H, a:a + G], kind)
+    k, v = k.to(dtype), v.to(dtype)
+    pool = sq.PagePool.empty(1, G, H, bits, G, meta_dtype=META[meta])
+    sq.squat_get_device_status()
+    sq.squat_pages_write(pool, torch.zeros(1, dtype=torch.int32, device="cuda"), k, v)
+    flags = sq.squat_get_device_status()
+    dk, dv = deq_pool(pool.tensors, bits, G)
+    for x, d, dim, exact in ((k, dk, 0, True), (v, dv, 2, False)):
+        code, scale, zero = (d[n][0].transpose(0, 1) for n in ("code", "scale", "zero"))                    # [G, H, D]
+        groups = x.float().unflatten(dim, (-1, G)) if dim else x.float().unsqueeze(0)
+        over = 3 if dim == 2 else 1
+        lo, hi = groups.amin(over, keepdim=True), groups.amax(over, keepdim=True)
+        for stored, grid in ((scale, (hi - lo) * torch.tensor(1.0 / L, dtype=torch.float32, device="cuda")), (zero, lo)):
+            grid = grid.to(META[meta]).expand_as(groups)
+            torch.testing.assert_close(stored, (grid.flatten(2, 3) if dim == 2 else grid[0]).double(), rtol=0, atol=0, equal_nan=True)
+        t = (x.double() - zero) / scale if exact else ((x.float() - zero.float()) / scale.float()).double()
+        ok = (scale > 0) & (scale < math.inf)
+        assert torch.equal(code, torch.where(ok, torch.round(t).clamp(0, L), 0.0))
+    want_flags = {"constant": sq.FLAG_ZERO_RANGE, "zero": sq.FLAG_ZERO_RANGE, "nan": sq.FLAG_NONFINITE, "inf": sq.FLAG_NONFINITE, "-inf": sq.FLAG_NONFINITE, "infinite range": sq.FLAG_NONFINITE}
+    if meta == "f32":
+        assert flags == want_flags.get(kind, 0)
