@@ -473,7 +473,7 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
  * in other company may differ in the last bit.
  * Everything that changes from step to step is read on the device, so a captured call can be replayed with other lengths,
  * pages and row ranges (n_q, n_seqs and max_q as captured).  A length or row range outside its limits sets SQUAT_FLAG_PAGES and is
- * cut to them; for a page number outside the pool (the flag too) the result of that sequence is not defined.
+ * cut to them; for a page number outside the pool (the flag too) no page is read, and the result of that sequence is not defined.
  * Scores, softmax and sums are float32.  Keys, values, queries and weights enter the tensor cores in binary16 (11 significant
  * bits: codes, bf16 rows and queries exactly, dequantized values and weights rounded) where their magnitudes allow it, else in
  * bf16.

@@ -466,23 +466,28 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
 
     // ---- cached steps
     const int steps = max(min(tb, ct) - ta, 0);
-    long long page_tok = 0;                          // lane i: where the tokens of step 32 b + i are
+    long long page_tok = 0;                          // lane i: where the tokens of step 32 b + i are; -1: on a page outside the pool
     auto look_up = [&](int first) {
         const int i = first + lane;
         if (i < steps) {
             const int t = (ta + i) * STEP, at = t / p.pool.page_tokens;
-            int page = __ldg(p.page_table + (long long)pl.seq * p.table_stride + at);
+            const int page = __ldg(p.page_table + (long long)pl.seq * p.table_stride + at);
             if ((unsigned)page >= (unsigned)p.pool.n_pages) {
                 atomicOr(p.status, SQUAT_FLAG_PAGES);
-                page = 0;
-            }
-            page_tok = (long long)page * p.pool.page_stride + (long long)pl.h * p.pool.head_stride + (t - at * p.pool.page_tokens);
+                page_tok = -1;
+            } else page_tok = (long long)page * p.pool.page_stride + (long long)pl.h * p.pool.head_stride + (t - at * p.pool.page_tokens);
         }
     };
     const unsigned stage0 = smem_u32(stages);
     auto load = [&](int i) {                         // step i into its stage
         if (i < steps) {
             const long long tok = __shfl_sync(0xffffffffu, page_tok, i & 31);
+            if (tok < 0) {                           // no page of anybody's is read: keys and values of zero
+#pragma unroll 1
+                for (int j = lane; j < S::BYTES / 16; j += 32) reinterpret_cast<uint4 *>(stages + i % STAGES * S::BYTES)[j] = make_uint4(0, 0, 0, 0);
+                cp_commit();
+                return;
+            }
             const unsigned dst = stage0 + i % STAGES * S::BYTES;
             const unsigned char *kc = p.pool.kc + tok * S::ROW, *vc = p.pool.vc + tok * S::ROW;
 #pragma unroll

@@ -509,15 +509,16 @@ __device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk 
 {
     using S = Plan<TILES>;
     const int row0_sm = 32 * group32 + pr.sub;
-    // the first of the thread's 32 tokens of a tile in the pool; -1: past the cached tokens
+    // the first of the thread's 32 tokens of a tile in the pool; -1: past the cached tokens, or on a page outside the pool (keys and
+    // values of zero in their place)
     auto place = [&](int t) -> long long {
         const int tk = t * T + 32 * group32;
         if (t >= min(sg.tb, sg.ct) || tk >= w.sq.cached) return -1;
         const int pg = tk / p.pool.page_tokens;
-        int page = __ldg(p.page_table + (long long)w.pl.seq * p.table_stride + pg);
+        const int page = __ldg(p.page_table + (long long)w.pl.seq * p.table_stride + pg);
         if ((unsigned)page >= (unsigned)p.pool.n_pages) {
             atomicOr(p.status, SQUAT_FLAG_PAGES);
-            page = 0;
+            return -1;
         }
         return (long long)page * p.pool.page_stride + (long long)w.pl.h * p.pool.head_stride + (tk - pg * p.pool.page_tokens);
     };
@@ -547,7 +548,7 @@ __device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk 
             if (tok >= 0) pr.template store_keys<BF>(k_to, row0_sm, ks_top, kz_top);
             else
 #pragma unroll
-                for (int i = 0; i < UNITS; ++i) store_unit(k_to, row0_sm + APART * i, pr.unit, zero);         // behind the last cached token
+                for (int i = 0; i < UNITS; ++i) store_unit(k_to, row0_sm + APART * i, pr.unit, zero);
             fence_async_smem();
             mbar_arrive(smem_u32(&sh.k_full[stage]));
             if (next >= 0) pr.load_keys(p.pool, next);

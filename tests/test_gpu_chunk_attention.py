@@ -313,3 +313,28 @@ def test_calls_at_the_same_time():
             sq.squat_chunk_attention(b.q, pool, b.q_start, b.cached, b.page_table, out, ws, b.max_q, b.k_new, b.v_new, b.new_start, b.new_len, stream=st)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+@pytest.mark.parametrize("bits, G, meta", [(2, 32, "f32"), (4, 64, "f16")])
+@pytest.mark.parametrize("nq", [1, 5, 40])
+def test_a_page_outside_the_pool_is_not_read(bits, G, meta, nq):
+    """Page 0 is no sequence's and holds NaN: the result stays finite."""
+    b = Batch(5 + nq, [(nq, 4 * G, nq + 2), (1, 3 * G, 2), (nq, 0, nq)], 4, 2, bits, G, meta, pages_of=1)
+    ref, _, bound = b.expected()
+    t = []
+    for x in b.tensors:
+        first = torch.zeros_like(x[:1])
+        t.append(torch.cat((first.fill_(math.nan if x.is_floating_point() else 255), x)))
+    b.tensors = t
+    b.page_table = torch.where(b.page_table >= 0, b.page_table + 1, b.page_table)
+    n = b.tensors[0].shape[0]
+    sq.squat_get_device_status()
+    for at in range(4):
+        for bad in (-1, n, 2 ** 31 - 1, -2 ** 31):
+            old = int(b.page_table[0, at])
+            b.page_table[0, at] = bad
+            out, lse = call(b)
+            assert sq.squat_get_device_status() == sq.FLAG_PAGES
+            assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+            assert bool(((out.double() - ref)[nq:].abs() <= (bound + 2.0 ** -8 * ref.abs())[nq:]).all())
+            b.page_table[0, at] = old
