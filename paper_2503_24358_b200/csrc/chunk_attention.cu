@@ -71,8 +71,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
 
 // What a lane has seen of the magnitudes.
 struct Range {
-    __half2 meta;                                    // largest of the values' scales and zero-points
-    float k, v;                                      // largest finite ones among rows in full precision
+    float k;                                         // largest finite one among keys in full precision
+    float v;                                         // largest of the values' scales and zero-points, and of the finite ones in full precision
     float score;                                     // largest score of cached tokens
     int odd_first, odd_last;                         // range of rows in full precision with infinities or NaN among their values
 };
@@ -292,6 +292,7 @@ __device__ __forceinline__ void cached_step(unsigned char *st, const CodeBias<BI
             const int at = (t * D + 16 * g) >> g_shift;
             sc[j] = meta_at<M16>(st + S::VS, at);
             zr[j] = meta_at<M16>(st + S::VZ, at);
+            if (!BF) range.v = fmaxf(range.v, fmaxf(fabsf(sc[j]), fabsf(zr[j])));      // (as stored: binary16 may make zeros of them)
         }
         __half2 s2[2], z2[2];
         uint32_t both[2][BITS];                      // halves of the words of two tokens
@@ -300,7 +301,6 @@ __device__ __forceinline__ void cached_step(unsigned char *st, const CodeBias<BI
             for (int e = 0; e < 2; ++e) {
                 s2[e] = __floats2half2_rn(sc[2 * e], sc[2 * e + 1]);
                 z2[e] = __floats2half2_rn(zr[2 * e], zr[2 * e + 1]);
-                range.meta = __hmax2(range.meta, __hmax2(__habs2(s2[e]), __habs2(z2[e])));
 #pragma unroll
                 for (int i = 0; i < BITS; ++i) both[e][i] = pair16(w[2 * e][i / 2], w[2 * e + 1][i / 2], i);
             }
@@ -587,9 +587,7 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) wide |= !(fabsf(acc.o[t][i][e]) < INFINITY) && acc.m[t][e & 1] < INFINITY;      // (a row with an infinite score of its own has no sum)
-    const float2 meta = __half22float2(range.meta);
-    const float v_low = fmaxf(fmaxf(meta.x, meta.y), range.v);
-    return __any_sync(0xffffffffu, wide) || (!__any_sync(0xffffffffu, v_low >= 0x1p-8f) && __any_sync(0xffffffffu, v_low > 0.0f));
+    return __any_sync(0xffffffffu, wide) || (!__any_sync(0xffffffffu, range.v >= 0x1p-8f) && __any_sync(0xffffffffu, range.v > 0.0f));
 }
 
 template <int BITS, bool M16, int NT>

@@ -224,15 +224,15 @@ struct Producer {
         }
     }
     template <bool BF>
-    __device__ __forceinline__ void store_values(unsigned char *to, int row, __half2 &s_top, __half2 &z_top) const
+    __device__ __forceinline__ void store_values(unsigned char *to, int row, float &s_top, float &z_top) const
     {
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
             uint32_t y[8];
             if (!BF) {
                 const __half2 s2 = __float2half2_rn(vs[i]), z2 = __float2half2_rn(vz[i]);
-                s_top = __hmax2(s_top, __habs2(s2));
-                z_top = __hmax2(z_top, __habs2(z2));
+                s_top = fmaxf(s_top, fabsf(vs[i]));      // (as stored: binary16 may make zeros of them)
+                z_top = fmaxf(z_top, fabsf(vz[i]));
 #pragma unroll
                 for (int m = 0; m < 8; ++m) y[m] = as_u32(__hfma2(pair(1, i, m), s2, z2));
             } else {
@@ -522,15 +522,15 @@ __device__ __forceinline__ void producer_tiles(const ChunkParams &p, const Walk 
         }
         return (long long)page * p.pool.page_stride + (long long)w.pl.h * p.pool.head_stride + (tk - pg * p.pool.page_tokens);
     };
-    __half2 ks_top = __float2half2_rn(0.0f), kz_top = ks_top, vs_top = ks_top, vz_top = ks_top;
-    float k_top = 0.0f, v_top = 0.0f;
+    __half2 ks_top = __float2half2_rn(0.0f), kz_top = ks_top;
+    float k_top = 0.0f, v_top = 0.0f, vs_top = 0.0f, vz_top = 0.0f;
     // what the segment's magnitudes were: before the last tile is handed on, so that who waits for its sums knows them
     auto publish = [&]() {
         if (BF) return;
         constexpr float L = float((1 << BITS) - 1);
         auto top = [](__half2 x) { const float2 f = __half22float2(x); return fmaxf(f.x, f.y); };
         atomicMax(&sh.k_top, __float_as_int(fmaxf(fmaf(L, top(ks_top), top(kz_top)), k_top)));
-        atomicMax(&sh.v_top, __float_as_int(fmaxf(fmaf(L, top(vs_top), top(vz_top)), v_top)));
+        atomicMax(&sh.v_top, __float_as_int(fmaxf(fmaf(L, vs_top, vz_top), v_top)));
     };
     long long tok = place(sg.ta), next = place(sg.ta + 1);
     if (tok >= 0) {

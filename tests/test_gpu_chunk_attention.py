@@ -338,3 +338,17 @@ def test_a_page_outside_the_pool_is_not_read(bits, G, meta, nq):
             assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
             assert bool(((out.double() - ref)[nq:].abs() <= (bound + 2.0 ** -8 * ref.abs())[nq:]).all())
             b.page_table[0, at] = old
+
+
+@pytest.mark.parametrize("v_size", [1e-6, 1e-9, 1e-20])
+@pytest.mark.parametrize("nq, rows", [(1, 0), (2, 0), (5, 0), (40, 0), (1, 40), (40, 70)])
+@pytest.mark.parametrize("bits, G", [(2, 32), (4, 64)])
+def test_values_below_binary16(v_size, nq, rows, bits, G):
+    """Scales and zero-points that binary16 would round to zero (below 2^-25), in segments without and with rows in full precision:
+    done in bf16, within the bounds of test_magnitudes_beyond_binary16."""
+    b = Batch(3, [(nq, 6 * G, rows)], 4, 1, bits, G, v_size=v_size, causal=False)
+    out, lse = call(b)
+    ref, ref_lse, bound = b.expected()
+    assert bool(((out.double() - ref).abs() <= 8 * bound + 2.0 ** -8 * ref.abs()).all())
+    assert ((out.double() - ref).norm() / ref.norm()).item() <= 2.0 ** -8 * 8 ** 0.5
+    assert (lse.double() - ref_lse).abs().max().item() <= 0.02 * 8
