@@ -22,8 +22,8 @@
 // 64 sequences of up to 4096 tokens, one new token each, 32 heads with keys of their own, 2 bits: 233 us, 2.6 TB/s of codes and metadata; the issue slots bound it
 // (790 instructions for 32 tokens of a head).
 // Binary16 keeps 11 significant bits, three more than bf16: the result's own rounding to bf16 is what is left.  Magnitudes
-// beyond its range (or values that all lie below 2^-8, where it would lose them) are noticed on the way, and the
-// segment is done again with bf16 operands.  Weights carry a factor of 2^8, so that those down to 2^-32 of the largest are not lost.
+// beyond its range (or values that all lie below 2^-8, where it would lose them, or keys and queries of which it would lose what
+// matters: chunk_too_low) are noticed on the way, and the segment is done again with bf16 operands.  Weights carry a factor of 2^8, so that those down to 2^-32 of the largest are not lost.
 #include "chunk_attention.cuh"
 
 namespace {
@@ -71,6 +71,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
 
 // What a lane has seen of the magnitudes.
 struct Range {
+    __half2 ks, kz;                                  // largest of the keys' scales and of their zero-points
     float k;                                         // largest finite one among keys in full precision
     float v;                                         // largest of the values' scales and zero-points, and of the finite ones in full precision
     float score;                                     // largest score of cached tokens
@@ -144,7 +145,7 @@ __device__ __forceinline__ void softmax_step(Acc<NT> &acc, float (&s)[NT][2][4],
 // lane makes one of them for the eight lanes that use it.
 constexpr int PAIRS_QUARTER = 8 * 16 + 16;           // padded: the four quarters fall on distinct banks
 template <int BITS, bool M16>
-__device__ __forceinline__ void order_key_meta(unsigned char *st)
+__device__ __forceinline__ void order_key_meta(unsigned char *st, Range &range)
 {
     using S = Stage<BITS, M16>;
     constexpr int HALF = BITS == 2 ? 8 : 4;          // codes in half a word; a pair is (c, c + HALF) of a word
@@ -163,6 +164,8 @@ __device__ __forceinline__ void order_key_meta(unsigned char *st)
             y[2 * e + 1] = pack16<false>(a.y, b.y);
         }
     }
+    range.ks = __hmax2(range.ks, __hmax2(__habs2(as_half2(y[0])), __habs2(as_half2(y[1]))));
+    range.kz = __hmax2(range.kz, __hmax2(__habs2(as_half2(y[2])), __habs2(as_half2(y[3]))));
     __syncwarp();
     *reinterpret_cast<uint4 *>(st + S::KS + quarter * PAIRS_QUARTER + (lane & 7) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
     __syncwarp();
@@ -172,6 +175,10 @@ __device__ __forceinline__ float meta_at(const unsigned char *from, int i)
 {
     return M16 ? __half2float(reinterpret_cast<const __half *>(from)[i]) : reinterpret_cast<const float *>(from)[i];
 }
+
+// For few rows it is less to scale the queries than the codes (16 products a row of eight rather than 128 differences and multiply-adds).
+template <int NT>
+constexpr bool folds = NT <= 2;
 
 // A step of cached tokens, staged at `st`.
 template <int BITS, bool M16, int NT, bool BF>
@@ -187,9 +194,8 @@ __device__ __forceinline__ void cached_step(unsigned char *st, const CodeBias<BI
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[t][k][e] = 0.0f;
-    if (!BF) order_key_meta<BITS, M16>(st);
-    // For few rows it is less to scale the queries than the codes (16 products a row of eight rather than 128 differences and multiply-adds)
-    constexpr bool FOLD = !BF && NT <= 2;
+    if (!BF) order_key_meta<BITS, M16>(st, range);
+    constexpr bool FOLD = !BF && folds<NT>;
     {
         float alike[NT][4];
         if (FOLD)
@@ -522,10 +528,11 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
     // ---- queries: rows 8 t + g, channels 32 q .. + 31, in the order of the key operand
     Queries<NT> queries;
     queries.smem = q_sm + 4 * lane;
-    float q_max = 0.0f;
+    float q_max = 0.0f, q_low = INFINITY;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int r = row0 + 8 * t + g;
+        float q_row = 0.0f;
         uint32_t x[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -539,9 +546,15 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
             const int lo = m / HALF * 2 * HALF + m % HALF;
             y[m] = pair16(x[lo / 2], x[(lo + HALF) / 2], lo);
             if (!BF) {
-                q_max = fmaxf(q_max, fmaxf(fabsf(bf16lo_to_f32(y[m])), fabsf(bf16hi_to_f32(y[m]))));
+                q_row = fmaxf(q_row, fmaxf(fabsf(bf16lo_to_f32(y[m])), fabsf(bf16hi_to_f32(y[m]))));
                 y[m] = bf16_pair_to_f16(y[m]);
             }
+        }
+        if (!BF) {
+            q_row = fmaxf(q_row, __shfl_xor_sync(0xffffffffu, q_row, 1));
+            q_row = fmaxf(q_row, __shfl_xor_sync(0xffffffffu, q_row, 2));
+            q_max = fmaxf(q_max, q_row);
+            if (q_row > 0.0f) q_low = fminf(q_low, q_row);
         }
         queries.put(t, y);
     }
@@ -578,9 +591,13 @@ __device__ __forceinline__ bool run_segment(const ChunkParams &p, const ChunkPla
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) acc.l[t][r] += __shfl_xor_sync(0xffffffffu, acc.l[t][r], o);
     if (BF) return false;
-    // Dequantized keys and values beyond binary16 have become infinities, and so have scores or sums.  Queries below 2^12: what falls
-    // below 2^-25 of a key's scale or zero-point is then less than 2^-13 of a score's unit even in 128 products.
-    bool wide = !(q_max < 4096.0f) || !(range.k < 65000.0f) || !(range.score < INFINITY);
+    // Dequantized keys and values beyond binary16 have become infinities, and so have scores or sums.  Queries count as beyond it from 2^12
+    // on, as in the kernel for many rows.
+    constexpr float L = float((1 << BITS) - 1);
+    const float2 ks = __half22float2(range.ks), kz = __half22float2(range.kz);
+    const float k_top = warp_max(fmaxf(fmaf(L, fmaxf(ks.x, ks.y), fmaxf(kz.x, kz.y)), range.k));
+    bool wide = chunk_too_low(p, folds<NT>, warp_max(q_max), warp_min(q_low), k_top);
+    wide |= !(q_max < 4096.0f) || !(range.k < 65000.0f) || !(range.score < INFINITY);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -822,6 +839,7 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
     p.G = pool->group_size;
     p.H = pool->n_kv_heads;
     p.qpk = p.Hq / p.H;
+    p.levels = (float)(1 << pool->bits);
     p.status = squat_status_word();
     if (!p.status) return SQUAT_ERR_CUDA;
     const ChunkKernels k = kernels_for(p.n_q, p.n_seqs, max_q, p.qpk);

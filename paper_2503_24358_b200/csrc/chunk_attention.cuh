@@ -23,6 +23,7 @@ struct ChunkParams {
     const __nv_bfloat16 *k_new, *v_new;
     long long knt, knh, vnt, vnh;
     float scale_log2;                                // softmax scale / ln 2
+    float levels;                                    // of a code: L + 1
     int min_rows, max_rows;                          // the kernel's sequences: those with so many rows
     int n_workers, min_tiles, start;                 // who share the work, the least that one takes, and what an item costs besides its tiles
     float *part, *ml;                                // [2 n_workers][R][D], [2 n_workers][R][2]
@@ -221,5 +222,17 @@ __device__ __forceinline__ float code_float(uint32_t word, int pos) { return (fl
 __device__ __forceinline__ uint32_t bf16_pair_to_f16(uint32_t x) { return pack16<false>(bf16lo_to_f32(x), bf16hi_to_f32(x)); }
 __device__ __forceinline__ bool bf16_pair_not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
+// Whether scores may have lost digits in binary16 that bf16 operands keep.  Below 2^-14 binary16 rounds by up to 2^-25 however small the
+// number is: a key's scale (times a code of at most L) and zero-point, a query, and with `fold` the product of a query and a scale.  Over
+// 128 channels an exponent is off by `off` at most; q_top: the largest query, k_top: L times the largest scale and the largest
+// zero-point together (or the largest key in full precision).  Where that matters, bf16, whose keys are off by 2^-9 of themselves, is
+// the better choice once the largest key, the largest channel of a query (q_low: the smallest such one among the rows, zeros apart) or
+// their product is so small that 2^-25, L + 1 times for a key, is more than 2^-9 of it: below (L + 1) 2^-16, for k_top, which may be
+// four times the largest key, (L + 1) 2^-14.
+__device__ __forceinline__ bool chunk_too_low(const ChunkParams &p, bool fold, float q_top, float q_low, float k_top)
+{
+    const float off = p.scale_log2 * 128.0f * 0x1p-25f * (p.levels * q_top + k_top + (fold ? p.levels : 0.0f)), least = p.levels * 0x1p-14f;
+    return !(off <= 0x1p-9f) && (k_top < least || q_low < 0x1p-16f || (fold && q_low * k_top < least));
+}
 
 int squat_launch_chunk_matrix(const ChunkParams &p, int tiles, int bits, int meta16, cudaStream_t st);

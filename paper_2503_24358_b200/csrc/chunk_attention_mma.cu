@@ -87,7 +87,7 @@ struct Shared {
     int failed;                                      // a bounded wait ran out: no more waits, the results are not valid
     int wide;                                        // binary16 is too narrow for the segment
     int odd_first, odd_last;                         // range of rows in full precision that hold infinities or NaN among their values
-    int v_top, k_top;                                // largest magnitudes, as float bits
+    int v_top, k_top, q_top, q_low;                  // largest magnitudes, as float bits; q_low: the smallest of the rows' largest
     ChunkShared place;
 };
 
@@ -290,22 +290,25 @@ __device__ __forceinline__ void segment_begins(Shared<TILES> &sh)
         sh.wide = 0;
         sh.odd_first = 0x7fffffff;
         sh.odd_last = -1;
-        sh.v_top = sh.k_top = 0;
+        sh.v_top = sh.k_top = sh.q_top = 0;
+        sh.q_low = 0x7f800000;
     }
     __syncthreads();
 }
 template <int TILES>
-__device__ __forceinline__ bool too_wide(Shared<TILES> &sh, bool bf)
+__device__ __forceinline__ bool too_wide(const ChunkParams &p, Shared<TILES> &sh, bool bf)
 {
+    if (bf) return false;
+    const float q_top = __int_as_float(*(volatile int *)&sh.q_top), q_low = __int_as_float(*(volatile int *)&sh.q_low);
     const float k_top = __int_as_float(*(volatile int *)&sh.k_top), v_top = __int_as_float(*(volatile int *)&sh.v_top);
-    return !bf && (*(volatile int *)&sh.wide || !(k_top < 4096.0f) || !(v_top < 65000.0f) || (v_top < 0x1p-8f && v_top > 0.0f));
+    return *(volatile int *)&sh.wide || !(k_top < 4096.0f) || !(v_top < 65000.0f) || (v_top < 0x1p-8f && v_top > 0.0f) || chunk_too_low(p, false, q_top, q_low, k_top);
 }
 template <int TILES>
-__device__ __forceinline__ bool segment_again(Shared<TILES> &sh, bool bf)
+__device__ __forceinline__ bool segment_again(const ChunkParams &p, Shared<TILES> &sh, bool bf)
 {
     __syncthreads();
     tc_fence_after();
-    const bool again = too_wide(sh, bf);
+    const bool again = too_wide(p, sh, bf);
     __syncthreads();
     return again;
 }
@@ -438,6 +441,11 @@ __device__ __forceinline__ void softmax_role(const ChunkParams &p, Walk w, Share
                     *reinterpret_cast<uint4 *>(base + (((u % 4 * 2 + 1) ^ (r & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
                 }
                 if (!(top < 4096.0f)) sh.wide = 1;
+                const float q_top = warp_max(top), q_low = warp_min(top > 0.0f ? top : INFINITY);
+                if (tid % 32 == 0) {
+                    atomicMax(&sh.q_top, __float_as_int(q_top));
+                    atomicMin(&sh.q_low, __float_as_int(q_low));
+                }
                 fence_async_smem();
             }
             __syncthreads();
@@ -448,7 +456,7 @@ __device__ __forceinline__ void softmax_role(const ChunkParams &p, Walk w, Share
                 else softmax_tiles<TILES, true>(p, sg, sh, w.sq.cached, sees, t, turns, s_addr, o_addr, m, l);
             wait_for(sh.o_full[t], segments & 1, sh.failed, p.status);
             tc_fence_after();
-            if (!too_wide(sh, bf)) {                 // (known: the last tile was handed on after it)
+            if (!too_wide(p, sh, bf)) {                 // (known: the last tile was handed on after it)
                     const bool whole = sg.ta == 0 && sg.tb == sg.tiles;
                     const long long slot = 2LL * blockIdx.x + (sg.ta == 0 ? 1 : 0);
                     const int row = sg.row0 + r, q_row = w.sq.q0 + row / p.qpk, hq = w.pl.h * p.qpk + row % p.qpk;
@@ -496,7 +504,7 @@ __device__ __forceinline__ void softmax_role(const ChunkParams &p, Walk w, Share
             tc_fence_before();
             turns += sg.n;
             ++segments;
-            if (!segment_again(sh, bf)) break;
+            if (!segment_again(p, sh, bf)) break;
         }
         walk_on<S::ROWS>(p, w, sg);
     }
@@ -627,7 +635,7 @@ __device__ __forceinline__ void producer_role(const ChunkParams &p, Walk w, Shar
                 else producer_tiles<BITS, G, M16, TILES, true>(p, w, sg, sh, pr, group32, kv, k_sm, v_sm);
             }
             kv += sg.n;
-            if (!segment_again(sh, bf)) break;
+            if (!segment_again(p, sh, bf)) break;
         }
         walk_on<S::ROWS>(p, w, sg);
     }
@@ -696,7 +704,7 @@ __device__ __forceinline__ void product_role(const ChunkParams &p, Walk w, Share
             }
             kv += sg.n;
             turns += sg.n;
-            if (!segment_again(sh, bf)) break;
+            if (!segment_again(p, sh, bf)) break;
         }
         walk_on<S::ROWS>(p, w, sg);
     }

@@ -352,3 +352,19 @@ def test_values_below_binary16(v_size, nq, rows, bits, G):
     assert bool(((out.double() - ref).abs() <= 8 * bound + 2.0 ** -8 * ref.abs()).all())
     assert ((out.double() - ref).norm() / ref.norm()).item() <= 2.0 ** -8 * 8 ** 0.5
     assert (lse.double() - ref_lse).abs().max().item() <= 0.02 * 8
+
+
+@pytest.mark.parametrize("q_size, k_size", [(600.0, 1e-4), (600.0, 1e-5), (600.0, 1e-7), (1.0, 1e-6), (1.0, 1e-9), (1e-3, 1e-3), (1e-6, 1.0), (1e-9, 1.0), (1e-9, 1e-9)])
+@pytest.mark.parametrize("nq, rows", [(1, 0), (2, 0), (5, 0), (40, 0), (1, 40), (40, 70)])
+@pytest.mark.parametrize("bits, G, meta", [(2, 32, "f32"), (4, 64, "f32"), (4, 64, "f16")])
+def test_keys_and_queries_below_binary16(q_size, k_size, nq, rows, bits, G, meta):
+    """Scores of ordinary size from keys or queries that binary16 would round to a few bits or to zero, with the softmax scale that
+    goes with them: done in bf16, within the bounds of test_magnitudes_beyond_binary16."""
+    if meta == "f16" and k_size < 1e-6:
+        k_size = 1e-6                                          # what such metadata can hold
+    b = Batch(3, [(nq, 6 * G, rows)], 4, 1, bits, G, meta, q_size=q_size, k_size=k_size, causal=False, scale=0.2 / (q_size * k_size))
+    out, lse = call(b)
+    ref, ref_lse, bound = b.expected()
+    assert bool(((out.double() - ref).abs() <= 8 * bound + 2.0 ** -8 * ref.abs()).all())
+    assert ((out.double() - ref).norm() / ref.norm()).item() <= 2.0 ** -8 * 8 ** 0.5
+    assert (lse.double() - ref_lse).abs().max().item() <= 0.02 * 8
