@@ -610,10 +610,15 @@ class RopePlan:
 _NO_ROWS = (None, 0, 0, 0, None, 0, 0)
 
 
-def _on_current_device(x, name):
-    """Kernels run on the current device, with its stream; memory of another one they could not reach."""
-    if x.is_cuda and x.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {x.device}, the current device is cuda:{torch.cuda.current_device()}")
+def _refuse_elsewhere(**tensors):
+    """Kernels run on the current device, with its stream; memory of another one, or of the host, they could not reach.  (Callers
+    compare device numbers and come here when one differs: a dict of a call's tensors costs as much as the comparison of all.)"""
+    here = torch.cuda.current_device()
+    for name, x in tensors.items():
+        if x is not None and x.get_device() < 0:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        if x is not None and x.get_device() != here:
+            raise ValueError(f"{name} is on cuda:{x.get_device()}, the current device is cuda:{here}")
 
 
 def _rows(x, name):
@@ -638,21 +643,24 @@ def squat_rope_apply(plan: RopePlan, positions: torch.Tensor, q: torch.Tensor = 
     x = q if q is not None else k
     if x is None:
         return
-    _on_current_device(x, "q")
     dtype = x.dtype
     T, _, d = x.shape
     if positions.shape != (plan.n_axes, T) or (T > 1 and positions.stride(1) != 1):
         raise ValueError("positions must be [n_axes, tokens] with contiguous tokens")
-    args = []
+    args, here, elsewhere = [], x.get_device(), False
     for a, b, name in ((q, q_out, "q"), (k, k_out, "k")):
         if a is None:
             args += _NO_ROWS
             continue
+        if a.get_device() != here or (b is not None and b.get_device() != here):
+            elsewhere = True
         shape = a.shape
         if a.dtype is not dtype or shape[0] != T or shape[2] != d or (b is not None and (b.shape != shape or b.dtype is not dtype)):
             raise ValueError("q, k and their outputs must have one dtype, token count and head_dim, and outputs their input's shape")
         pa = _rows(a, name)
         args += (pa[0], shape[1], pa[1], pa[2], *(pa if b is None else _rows(b, name)))
+    if here != torch.cuda.current_device() or positions.get_device() != here or elsewhere:
+        _refuse_elsewhere(positions=positions, q=q, k=k, q_out=q_out, k_out=k_out)
     _check(_direct().rope_apply(plan.address, _dev(positions, "positions"), p_dtype is torch.int64, positions.stride(0), T, d, _dtype_code(x),
                                 1 if inverse else 0, *args, _stream(stream)), "squat_rope_apply")
 
@@ -700,9 +708,13 @@ class PagePool:
         self.k_codes, self.k_scales, self.k_zeros, self.v_codes, self.v_scales, self.v_zeros = tensors
         self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, self.bits, self.group_size = n, P, H, d, bits, G
         self.device = k_codes.device
+        self._at = k_codes.get_device() if k_codes.numel() else None      # (what an empty pool holds is never read)
         names = ("k_codes", "k_scales", "k_zeros", "v_codes", "v_scales", "v_zeros")
         self._pool = PagePool._Struct(*(_dev(t, m) if t.numel() else None for t, m in zip(tensors, names)), ps, hs, n, P, H, d, bits, G, int(meta16))
         self.address = ctypes.addressof(self._pool)
+
+    def _device_of(self):
+        return self.k_codes if self._at is not None else None
 
     @classmethod
     def empty(cls, n_pages: int, page_tokens: int, n_kv_heads: int, bits: int, group_size: int, head_dim: int = 128,
@@ -721,12 +733,12 @@ def _int32(t, name, numel):
     return t.data_ptr()
 
 
-def _pool_rows(pool, slots, tensors, names):
+def _pool_rows(pool, slots, tensors, names, workspace=None):
     """Token count and dtype of the key and value rows that come with `slots`, and their addresses and strides."""
-    _on_current_device(slots, "slots")
     T = slots.numel() * pool.group_size
     want = (T, pool.n_kv_heads, pool.head_dim)
-    args, dtype = [], None
+    args, dtype, here = [], None, slots.get_device()
+    elsewhere = pool._at not in (None, here) or (workspace is not None and workspace.get_device() != here)
     for x, name in zip(tensors, names):
         if x is None:
             args += (None, 0, 0)
@@ -735,8 +747,12 @@ def _pool_rows(pool, slots, tensors, names):
             raise ValueError(f"{name} must be [len(slots) * group_size, n_kv_heads, head_dim]")
         if dtype is not None and x.dtype is not dtype:
             raise ValueError(f"{names[0]} and {names[1]} must have one dtype")
+        if x.get_device() != here:
+            elsewhere = True
         dtype = x.dtype
         args += _rows(x, name)
+    if dtype is not None and (elsewhere or here != torch.cuda.current_device()):
+        _refuse_elsewhere(slots=slots, pool=pool._device_of(), **dict(zip(names, tensors)), workspace=workspace)
     return T, dtype, args
 
 
@@ -749,7 +765,7 @@ def squat_pages_write(pool: PagePool, slots: torch.Tensor, k: torch.Tensor = Non
     """Quantizes k and / or v [tokens, n_kv_heads, d] into the pool: group i of group_size tokens goes to slots[i] (int32, page *
     page_tokens + token; negative: not written).  With a Subspace the keys are quantized with its error feedback, through a
     workspace (CUDA uint8) of squat_pages_write_workspace_bytes(pool, tokens); without one they are rounded to nearest."""
-    T, dtype, args = _pool_rows(pool, slots, (k, v), ("k", "v"))
+    T, dtype, args = _pool_rows(pool, slots, (k, v), ("k", "v"), workspace)
     if dtype is None:
         return
     x = k if k is not None else v
@@ -782,8 +798,7 @@ def squat_chunk_attention(q: torch.Tensor, pool: PagePool, q_start: torch.Tensor
     k_new / v_new[new_start[i]:][:new_len[i]] (bfloat16 [rows, n_kv_heads, d]).  Index tensors are int32 on the device and are
     read there; max_q is the largest number of queries of a sequence.  workspace: CUDA uint8 of
     squat_chunk_attention_workspace_bytes(n_q, n_q_heads, n_kv_heads, max_q)."""
-    _on_current_device(q, "q")
-    n_seqs, bf16, shape, d = cached_len.numel(), torch.bfloat16, q.shape, pool.head_dim
+    n_seqs, bf16, shape, d, here = cached_len.numel(), torch.bfloat16, q.shape, pool.head_dim, q.get_device()
     if len(shape) != 3 or shape != out.shape or q.dtype is not bf16 or out.dtype is not bf16 or shape[2] != d:
         raise ValueError("q and out must be bfloat16 [n_q, n_q_heads, head_dim]")
     table = page_table.shape
@@ -800,6 +815,11 @@ def squat_chunk_attention(q: torch.Tensor, pool: PagePool, q_start: torch.Tensor
         (pk, kt, kh), (pv, vt, vh) = _rows(k_new, "k_new"), _rows(v_new, "v_new")
         rows = (pk, pv, n_new, kt, kh, vt, vh)
         starts = (_int32(new_start, "new_start", n_seqs), _int32(new_len, "new_len", n_seqs))
+        if not (here == k_new.get_device() == v_new.get_device() == new_start.get_device() == new_len.get_device()):
+            _refuse_elsewhere(k_new=k_new, v_new=v_new, new_start=new_start, new_len=new_len, q=q)
+    if not (here == q_start.get_device() == cached_len.get_device() == page_table.get_device() == out.get_device() == workspace.get_device() == torch.cuda.current_device()) or \
+            pool._at not in (None, here) or (lse is not None and lse.get_device() != here):
+        _refuse_elsewhere(q=q, pool=pool._device_of(), q_start=q_start, cached_len=cached_len, page_table=page_table, out=out, workspace=workspace, lse=lse)
     _check(_direct().chunk_attention(
         softmax_scale, *_q_rows(q, "q"), pool.address, n_seqs, _int32(q_start, "q_start", n_seqs + 1), _int32(cached_len, "cached_len", n_seqs),
         _int32(page_table, "page_table", n_seqs * table[1]), table[1], *rows, *starts, max_q, 1 if causal else 0, *_rows(out, "out"),

@@ -200,3 +200,69 @@ def test_more_tokens_than_32_bits_count(lib):
     assert attend(lib, width=(1 << 31) // pool().page_tokens) == UNSUPPORTED
     assert attend(lib, n_new=(1 << 31) - 1) == UNSUPPORTED
     assert rope(lib, hq=(1 << 31) - 1) == UNSUPPORTED
+
+
+class OnDevice(torch.Tensor):
+    """Host memory that says it is on a CUDA device (device 0 unless `at` is set)."""
+    at = 0
+    is_cuda = property(lambda self: True)
+
+    def get_device(self):
+        return self.at
+
+
+def _fake(*shape, dtype=torch.bfloat16):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnDevice)
+
+
+def _fake_calls():
+    """The four calls and the tensors that each takes, all on device 0."""
+    i32 = lambda *shape: _fake(*shape, dtype=torch.int32)  # noqa: E731
+    pool = lambda: [t.as_subclass(OnDevice) for t in _tensors()]  # noqa: E731
+    plan = sq.RopePlan()
+
+    def rope(**t):
+        sq.squat_rope_apply(plan, **t)
+
+    def on_pool(call, **t):
+        call(sq.PagePool(*(t.pop(f"pool{i}") for i in range(6))), **t)
+
+    def attention(**t):
+        p = sq.PagePool(*(t.pop(f"pool{i}") for i in range(6)))
+        sq.squat_chunk_attention(pool=p, max_q=1, **t)
+
+    pages = {f"pool{i}": t for i, t in enumerate(pool())}
+    rows = {n: _fake(64, 2, 128) for n in ("k", "v")}
+    yield rope, dict(positions=i32(1, 4), q=_fake(4, 2, 128), k=_fake(4, 2, 128), q_out=_fake(4, 2, 128), k_out=_fake(4, 2, 128))
+    yield lambda **t: on_pool(sq.squat_pages_write, **t), dict(pages, slots=i32(2), workspace=_fake(4096, dtype=torch.uint8), **rows)
+    yield lambda **t: on_pool(sq.squat_pages_read, **t), dict(pages, slots=i32(2), k_out=rows["k"], v_out=rows["v"])
+    yield attention, dict(pages, q=_fake(3, 4, 128), q_start=i32(3), cached_len=i32(2), page_table=i32(2, 1), out=_fake(3, 4, 128), workspace=_fake(4096, dtype=torch.uint8),
+                          k_new=_fake(5, 2, 128), v_new=_fake(5, 2, 128), new_start=i32(2), new_len=i32(2), lse=_fake(3, 4, dtype=torch.float32))
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """Each of a call's tensors on another device than the current one, or on the host, is refused before the library sees an address."""
+    seen = []
+
+    class Calls:
+        def __getattr__(self, name):
+            return lambda *args: seen.append(name) or 0
+
+    monkeypatch.setattr(sq.binding, "_direct", Calls)
+    monkeypatch.setattr(sq.binding, "_stream", lambda stream: None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for i, (call, tensors) in enumerate(_fake_calls()):
+        call(**tensors)
+        assert len(seen) == i + 1
+        for name, x in tensors.items():
+            if name.startswith("pool") and name != "pool0":
+                continue                                      # (the six have one device, which PagePool checks)
+            for at in (1, -1):
+                x.at = at
+                with pytest.raises(ValueError, match="cuda:1" if at == 1 else "CUDA"):
+                    call(**tensors)
+            del x.at
+        assert len(seen) == i + 1
+    # an empty pool is nowhere
+    call(**dict(tensors, **{f"pool{i}": t for i, t in enumerate(_tensors(n=0))}))
+    assert len(seen) == i + 2
