@@ -442,7 +442,8 @@ int squat_pages_write(const squat_subspace *s, const squat_page_pool *pool, cons
  * Reads groups of tokens back from pages (squat_dequantize with places): row i * group_size + t of k_out and v_out
  * [n_tokens, n_kv_heads, d] becomes the token at slots[i] + t.  Rows of a negative slot are left as they were, and so are those of a
  * slot outside the pool (SQUAT_FLAG_PAGES).  Either output may be NULL.  Element strides are multiples of 16 bytes; rows that
- * overlap are refused.
+ * overlap are refused, those of k_out with those of v_out too.  Rows of the two that lie between each other's (side by side in
+ * one tensor) need equal strides.
  */
 int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens, int out_dtype,
                      void *k_out, long long k_stride_t, long long k_stride_h,

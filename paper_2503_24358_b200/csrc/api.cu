@@ -722,6 +722,28 @@ int check_rows(const void *x, long long stride_t, long long stride_h, int n_toke
     return SQUAT_OK;
 }
 
+// Whether rows of a and of b, both [n_tokens, heads, D] of one type and apart among themselves, share memory.  Rows that lie between
+// each other's have to have equal strides: a difference of two rows then is one of `heads` and one of `tokens` steps, of which only
+// the nearest needs a look.
+bool rows_meet(const void *a, long long at, long long ah, const void *b, long long bt, long long bh, int n_tokens, int heads, int dtype)
+{
+    typedef __int128 wide;
+    const wide size = D, between = ((wide)reinterpret_cast<uintptr_t>(b) - (wide)reinterpret_cast<uintptr_t>(a)) / (wide)elem_size(dtype);      // (both 16-byte aligned)
+    if (n_tokens == 1) at = bt = 0;
+    if (heads == 1) ah = bh = 0;
+    auto extent = [&](long long t, long long h) { return (wide)(n_tokens - 1) * t + (wide)(heads - 1) * h + size; };
+    if (between >= extent(at, ah) || -between >= extent(bt, bh)) return false;
+    if (at != bt || ah != bh) return true;
+    for (int dh = 1 - heads; dh < heads; ++dh) {
+        const wide x = between + (wide)dh * ah;
+        wide dt = at ? (x >= 0 ? x + at / 2 : x - at / 2) / at : 0;
+        dt = dt > n_tokens - 1 ? n_tokens - 1 : dt < 1 - n_tokens ? 1 - n_tokens : dt;
+        const wide off = x - dt * at;
+        if (off < size && -off < size) return true;
+    }
+    return false;
+}
+
 struct PagesWriteLayout {
     size_t codes, scales, zeros, total;
 };
@@ -790,6 +812,7 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
     if (k_out && (rc = check_rows(k_out, k_stride_t, k_stride_h, n_tokens, pool->n_kv_heads, out_dtype, true)) != SQUAT_OK) return rc;
     if (v_out && (rc = check_rows(v_out, v_stride_t, v_stride_h, n_tokens, pool->n_kv_heads, out_dtype, true)) != SQUAT_OK) return rc;
     if (n_tokens == 0 || (!k_out && !v_out)) return SQUAT_OK;
+    if (k_out && v_out && rows_meet(k_out, k_stride_t, k_stride_h, v_out, v_stride_t, v_stride_h, n_tokens, pool->n_kv_heads, out_dtype)) return SQUAT_ERR_INVALID_ARG;
     if (!slots || !aligned4(slots)) return SQUAT_ERR_INVALID_ARG;
     unsigned *status = squat_status_word();
     if (!status) return SQUAT_ERR_CUDA;

@@ -315,3 +315,32 @@ def test_odd_groups_leave_their_neighbours_alone(kind, dtype, meta, bits, G):
     want_flags = {"constant": sq.FLAG_ZERO_RANGE, "zero": sq.FLAG_ZERO_RANGE, "nan": sq.FLAG_NONFINITE, "inf": sq.FLAG_NONFINITE, "-inf": sq.FLAG_NONFINITE, "infinite range": sq.FLAG_NONFINITE}
     if meta == "f32":
         assert flags == want_flags.get(kind, 0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_keys_and_values_read_into_one_tensor(dtype):
+    """k_out and v_out may lie between each other's rows, but share none: refused exactly where two rows meet, else read in full."""
+    H, G = 3, 32
+    k, v, _ = inputs(8, G, H, torch.float32)
+    pool = sq.PagePool.empty(1, G, H, 2, G)
+    slots = torch.zeros(1, dtype=torch.int32, device="cuda")
+    sq.squat_pages_write(pool, slots, k, v)
+    ref = torch.empty((2, G, H, D), dtype=dtype, device="cuda")
+    sq.squat_pages_read(pool, slots, *ref)
+    found = {True: 0, False: 0}
+    for kt, kh in ((H * D, D), (2 * H * D, D), (2 * H * D, 2 * D), (D, G * D), (2 * D, 2 * G * D), (D + 8, G * (D + 8))):
+        span = (G - 1) * kt + (H - 1) * kh + D
+        rows = torch.tensor([t * kt + h * kh for t in range(G) for h in range(H)])
+        for at in [x * D for x in range(-2 * H * G, 2 * H * G + 1, 5)] + [D, -D, H * D, 8, -8, D - 8, D + 8, -D - 8, span, -span, span - 8, 8 - span]:
+            flat = torch.zeros(2 * span + abs(at), dtype=dtype, device="cuda")
+            a, b = (torch.as_strided(flat, (G, H, D), (kt, kh, 1), max(0, x)) for x in (-at, at))
+            meet = bool(((rows.unsqueeze(1) - rows - at).abs() < D).any())
+            found[meet] += 1
+            if meet:
+                with pytest.raises(sq.SquatError):
+                    sq.squat_pages_read(pool, slots, a, b)
+                assert not flat.any()
+            else:
+                sq.squat_pages_read(pool, slots, a, b)
+                assert torch.equal(a, ref[0]) and torch.equal(b, ref[1])
+    assert min(found.values()) > 100, found

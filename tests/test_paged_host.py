@@ -266,3 +266,13 @@ def test_tensors_of_another_device(monkeypatch):
     # an empty pool is nowhere
     call(**dict(tensors, **{f"pool{i}": t for i, t in enumerate(_tensors(n=0))}))
     assert len(seen) == i + 2
+
+
+def test_keys_and_values_that_are_read_into_one_place(lib):
+    row = 256                                                 # bytes of a bf16 row
+    assert read(lib, k=A, v=A) == INVALID                     # the same rows
+    assert read(lib, k=A, v=A + 7 * row) == INVALID           # one head on
+    assert read(lib, k=A + 63 * 1024 * 2, v=A) == INVALID     # the last token on the first, from either side
+    assert read(lib, k=A, v=A + 16) == INVALID                # a part of a row
+    assert read(lib, k=A, kt=2048, v=A + 2048, vt=1024) == INVALID      # between each other's, with other strides
+    assert read(lib, k=A, kt=2048, v=A + 2048 - 16, vt=2048) == INVALID
