@@ -39,7 +39,7 @@ struct Stage {                                       // one step's part of the c
     static constexpr int KC = 0, VC = STEP * ROW, KS = 2 * STEP * ROW, KZ = KS + 4 * QUARTER, VS = KZ + 4 * QUARTER, VZ = VS + STEP * 4 * MS;
     static constexpr int BYTES = VZ + STEP * 4 * MS;
 };
-// CTAs to an SM
+// CTAs to an SM, by registers
 template <int NT>
 constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;
 
@@ -768,10 +768,25 @@ __global__ void __launch_bounds__(D) chunk_combine_kernel(const __grid_constant_
 }
 
 template <int BITS, bool M16, int NT>
+constexpr int ROWS_SMEM = WARPS * (STAGES * Stage<BITS, M16>::BYTES + Queries<NT>::BYTES);
+// CTAs of an instance to an SM: as many as its registers allow, if shared memory (228 KB, 1 KB of it for every CTA) holds them.  (For 4-bit
+// codes with float32 metadata and 8 rows it holds three.  Work shared out among four of them: 64 ragged sequences of up to 4096 tokens x 32
+// heads 327 us, a quarter of the CTAs after the others; among three 285.)
+template <int BITS, bool M16, int NT>
+constexpr int FITTING = [] {
+    int n = CTAS<NT>;
+    while (n * (ROWS_SMEM<BITS, M16, NT> + (int)sizeof(ChunkShared) + 1024) > 228 * 1024) --n;
+    return n;
+}();
+template <int NT>
+int fitting(int bits, int meta16)
+{
+    return bits == 2 ? meta16 ? FITTING<2, true, NT> : FITTING<2, false, NT> : meta16 ? FITTING<4, true, NT> : FITTING<4, false, NT>;
+}
+template <int BITS, bool M16, int NT>
 int launch_rows(const ChunkParams &p, cudaStream_t st)
 {
-    using S = Stage<BITS, M16>;
-    constexpr size_t smem = WARPS * (STAGES * S::BYTES + Queries<NT>::BYTES);
+    constexpr int smem = ROWS_SMEM<BITS, M16, NT>;
     static std::atomic<unsigned long long> allowed{0};
     const int rc = squat_allow_smem(reinterpret_cast<const void *>(chunk_rows_kernel<BITS, M16, NT>), smem, allowed);
     if (rc != SQUAT_OK) return rc;
@@ -804,7 +819,11 @@ ChunkKernels kernels_for(long long n_q, long long n_seqs, long long max_q, int q
     if (k.tiles && (n_q == n_seqs * max_q || qpk > FEW_ROWS)) k.eights = 0;
     return k;
 }
-int rows_workers(int eights) { return WARPS * squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : CTAS<3>); }
+int rows_workers(int eights, int bits, int meta16)
+{
+    return WARPS * squat_sm_count() * (eights == 1 ? fitting<1>(bits, meta16) : eights == 2 ? fitting<2>(bits, meta16) : fitting<3>(bits, meta16));
+}
+int rows_workers(int eights) { return WARPS * squat_sm_count() * (eights == 1 ? CTAS<1> : eights == 2 ? CTAS<2> : CTAS<3>); }      // of any pool
 int matrix_workers(int tiles) { return squat_sm_count() * (tiles == 2 ? 1 : 2); }
 size_t part_floats(int workers, int rows) { return 2 * (size_t)workers * rows * (D + 2); }
 // Workers, at most as many as the longest sequences that the page table can hold would give work to, and their parts.
@@ -859,7 +878,7 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
         few.max_rows = k.tiles ? FEW_ROWS : 0x7fffffff;
         few.min_tiles = 3;
         few.start = 2;
-        use_part(few, workspace, rows_workers(k.eights), 8 * k.eights, STEP, WARPS);
+        use_part(few, workspace, rows_workers(k.eights, pool->bits, pool->meta16), 8 * k.eights, STEP, WARPS);
         switch (k.eights) {
             case 1: rc = launch_rows_tiles<1>(few, pool->bits, pool->meta16, st); break;
             case 2: rc = launch_rows_tiles<2>(few, pool->bits, pool->meta16, st); break;
