@@ -825,7 +825,7 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
 size_t squat_chunk_attention_workspace_bytes(int n_q, int n_q_heads, int n_kv_heads, int max_q)
 {
     if (n_q < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || max_q < 0) return 0;
-    return (squat_chunk_workspace_floats(n_q, n_q_heads, n_kv_heads, max_q) * sizeof(float) + 255) / 256 * 256;
+    return (squat_chunk_workspace_floats(n_q_heads, n_kv_heads, max_q) * sizeof(float) + 255) / 256 * 256;
 }
 
 int squat_chunk_attention(const void *q, int n_q, int n_q_heads, long long q_stride_t, long long q_stride_h,

@@ -838,16 +838,15 @@ void use_part(ChunkParams &p, float *at, int workers, int rows, int tile, int to
 template <int ROWS>
 int launch_combine(const ChunkParams &p, cudaStream_t st)
 {
-    if (ROWS >= 128) return squat_launch(chunk_combine_kernel<ROWS, 128, true>, dim3((unsigned)p.n_workers, ROWS / 16), D, 0, st, p);
     // (a CTA for every row that a decode step has; more rows than that in turns of four)
-    return squat_launch(chunk_combine_kernel<ROWS, STEP, false>, dim3((unsigned)p.n_workers, (unsigned)(p.qpk < ROWS / 4 ? p.qpk : ROWS / 4)), D, 0, st, p);
+    if constexpr (ROWS >= 128) return squat_launch(chunk_combine_kernel<ROWS, 128, true>, dim3((unsigned)p.n_workers, ROWS / 16), D, 0, st, p);
+    else return squat_launch(chunk_combine_kernel<ROWS, STEP, false>, dim3((unsigned)p.n_workers, (unsigned)(p.qpk < ROWS / 4 ? p.qpk : ROWS / 4)), D, 0, st, p);
 }
 
 }  // namespace
 
-size_t squat_chunk_workspace_floats(int n_q, int n_q_heads, int n_kv_heads, int max_q)
+size_t squat_chunk_workspace_floats(int n_q_heads, int n_kv_heads, int max_q)
 {
-    (void)n_q;
     const ChunkKernels k = kernels_for(-1, 1, max_q, n_q_heads / n_kv_heads);
     return part_floats(rows_workers(k.eights), 8 * k.eights) + (k.tiles ? part_floats(matrix_workers(k.tiles), 128 * k.tiles) : 0);
 }

@@ -449,57 +449,57 @@ __device__ __forceinline__ void softmax_role(const ChunkParams &p, Walk w, Share
                 fence_async_smem();
             }
             __syncthreads();
-                const unsigned s_addr = tmem + 128 * t + ((unsigned)(warp % 4 * 32) << 16), o_addr = tmem + 128 * (TILES + t) + ((unsigned)(warp % 4 * 32) << 16);
-                const int sees = chunk_sees(p, w.sq, min(sg.row0 + r, sg.last) / p.qpk);
-                float m, l;
-                if (!bf) softmax_tiles<TILES, false>(p, sg, sh, w.sq.cached, sees, t, turns, s_addr, o_addr, m, l);
-                else softmax_tiles<TILES, true>(p, sg, sh, w.sq.cached, sees, t, turns, s_addr, o_addr, m, l);
+            const unsigned s_addr = tmem + 128 * t + ((unsigned)(warp % 4 * 32) << 16), o_addr = tmem + 128 * (TILES + t) + ((unsigned)(warp % 4 * 32) << 16);
+            const int sees = chunk_sees(p, w.sq, min(sg.row0 + r, sg.last) / p.qpk);
+            float m, l;
+            if (!bf) softmax_tiles<TILES, false>(p, sg, sh, w.sq.cached, sees, t, turns, s_addr, o_addr, m, l);
+            else softmax_tiles<TILES, true>(p, sg, sh, w.sq.cached, sees, t, turns, s_addr, o_addr, m, l);
             wait_for(sh.o_full[t], segments & 1, sh.failed, p.status);
             tc_fence_after();
             if (!too_wide(p, sh, bf)) {                 // (known: the last tile was handed on after it)
-                    const bool whole = sg.ta == 0 && sg.tb == sg.tiles;
-                    const long long slot = 2LL * blockIdx.x + (sg.ta == 0 ? 1 : 0);
-                    const int row = sg.row0 + r, q_row = w.sq.q0 + row / p.qpk, hq = w.pl.h * p.qpk + row % p.qpk;
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                    const int odd_first = max(sh.odd_first, (max(sg.ta, sg.ct) - sg.ct) * T), odd_last = min(sh.odd_last, sees - 1);
+                const bool whole = sg.ta == 0 && sg.tb == sg.tiles;
+                const long long slot = 2LL * blockIdx.x + (sg.ta == 0 ? 1 : 0);
+                const int row = sg.row0 + r, q_row = w.sq.q0 + row / p.qpk, hq = w.pl.h * p.qpk + row % p.qpk;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                const int odd_first = max(sh.odd_first, (max(sg.ta, sg.ct) - sg.ct) * T), odd_last = min(sh.odd_last, sees - 1);
 #pragma unroll 1
-                    for (int b = 0; b < 4; ++b) {
-                        float x[32];
-                        __syncwarp();
-                        tmem_ld32(o_addr + 32 * b, x);
-                        tmem_ld_wait();
-                        if (r >= sg.n_rows) continue;
-                        float y[32];                 // in the order of the channels
+                for (int b = 0; b < 4; ++b) {
+                    float x[32];
+                    __syncwarp();
+                    tmem_ld32(o_addr + 32 * b, x);
+                    tmem_ld_wait();
+                    if (r >= sg.n_rows) continue;
+                    float y[32];                 // in the order of the channels
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int e = i % 16, at_reg = BITS == 2 ? 2 * (e % 8) + e / 8 : e / 8 * 8 + 2 * (e % 4) + e % 8 / 4;
+                        y[i] = l == 0.0f ? 0.0f : x[i / 16 * 16 + at_reg];
+                    }
+                    for (int u = odd_first; u <= odd_last; ++u) {       // rare: infinities and NaN that the row sees
+                        const __nv_bfloat16 *v = p.v_new + (long long)(w.sq.k0 + u) * p.vnt + (long long)w.pl.h * p.vnh + 32 * b;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            const int e = i % 16, at_reg = BITS == 2 ? 2 * (e % 8) + e / 8 : e / 8 * 8 + 2 * (e % 4) + e % 8 / 4;
-                            y[i] = l == 0.0f ? 0.0f : x[i / 16 * 16 + at_reg];
-                        }
-                        for (int u = odd_first; u <= odd_last; ++u) {       // rare: infinities and NaN that the row sees
-                            const __nv_bfloat16 *v = p.v_new + (long long)(w.sq.k0 + u) * p.vnt + (long long)w.pl.h * p.vnh + 32 * b;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                const float o = __bfloat162float(v[i]);
-                                if (!(fabsf(o) < INFINITY)) y[i] += o;
-                            }
-                        }
-                        if (whole) {
-                            uint32_t w[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) w[i] = pack16<true>(y[2 * i] * inv, y[2 * i + 1] * inv);
-                            uint4 *to = reinterpret_cast<uint4 *>(p.out + (long long)q_row * p.ot + (long long)hq * p.oh + 32 * b);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) to[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-                        } else {
-                            float4 *to = reinterpret_cast<float4 *>(p.part + (slot * S::ROWS + r) * D + 32 * b);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                            const float o = __bfloat162float(v[i]);
+                            if (!(fabsf(o) < INFINITY)) y[i] += o;
                         }
                     }
-                    if (r < sg.n_rows) {
-                        if (!whole) *reinterpret_cast<float2 *>(p.ml + (slot * S::ROWS + r) * 2) = make_float2(m, l);
-                        else if (p.lse) p.lse[(long long)q_row * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
+                    if (whole) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) w[i] = pack16<true>(y[2 * i] * inv, y[2 * i + 1] * inv);
+                        uint4 *to = reinterpret_cast<uint4 *>(p.out + (long long)q_row * p.ot + (long long)hq * p.oh + 32 * b);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) to[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                    } else {
+                        float4 *to = reinterpret_cast<float4 *>(p.part + (slot * S::ROWS + r) * D + 32 * b);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
                     }
+                }
+                if (r < sg.n_rows) {
+                    if (!whole) *reinterpret_cast<float2 *>(p.ml + (slot * S::ROWS + r) * 2) = make_float2(m, l);
+                    else if (p.lse) p.lse[(long long)q_row * p.Hq + hq] = l == 0.0f ? -INFINITY : (m - P_SHIFT + log2f(l)) * 0.6931471805599453f;
+                }
             }
             tc_fence_before();
             turns += sg.n;
@@ -630,10 +630,8 @@ __device__ __forceinline__ void producer_role(const ChunkParams &p, Walk w, Shar
         for (bool bf = false;; bf = true) {
             segment_begins(sh);
             __syncthreads();
-            {
-                if (!bf) producer_tiles<BITS, G, M16, TILES, false>(p, w, sg, sh, pr, group32, kv, k_sm, v_sm);
-                else producer_tiles<BITS, G, M16, TILES, true>(p, w, sg, sh, pr, group32, kv, k_sm, v_sm);
-            }
+            if (!bf) producer_tiles<BITS, G, M16, TILES, false>(p, w, sg, sh, pr, group32, kv, k_sm, v_sm);
+            else producer_tiles<BITS, G, M16, TILES, true>(p, w, sg, sh, pr, group32, kv, k_sm, v_sm);
             kv += sg.n;
             if (!segment_again(p, sh, bf)) break;
         }

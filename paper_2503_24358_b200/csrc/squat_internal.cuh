@@ -151,7 +151,7 @@ int squat_launch_pages(bool write, const squat_page_pool *pool, const int *slots
                        const void *const (&x)[2], void *const (&y)[2], const long long (&strides)[2][2], unsigned *status, cudaStream_t st);
 int squat_launch_pages_place(const squat_page_pool *pool, const int *slots, int n_groups, const void *codes, const void *scales,
                              const void *zeros, unsigned *status, cudaStream_t st);
-size_t squat_chunk_workspace_floats(int n_q, int n_q_heads, int n_kv_heads, int max_q);
+size_t squat_chunk_workspace_floats(int n_q_heads, int n_kv_heads, int max_q);
 int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, float *workspace, int max_q, cudaStream_t st);
 
 // ---- the bounds-checked build ----------------------------------------------------------
