@@ -756,6 +756,13 @@ def _pool_rows(pool, slots, tensors, names, workspace=None):
     return T, dtype, args
 
 
+def _space(workspace):
+    """Address and bytes of a workspace."""
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
 def squat_pages_write_workspace_bytes(pool: PagePool, n_tokens: int) -> int:
     return int(_load().squat_pages_write_workspace_bytes(pool.address, n_tokens))
 
@@ -770,9 +777,7 @@ def squat_pages_write(pool: PagePool, slots: torch.Tensor, k: torch.Tensor = Non
         return
     x = k if k is not None else v
     _check(_direct().pages_write(None if s is None else s.handle.value, pool.address, _int32(slots, "slots", slots.numel()), T, _dtype_code(x),
-                                     *args, None if workspace is None else _dev(workspace, "workspace"),
-                                     0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
-           "squat_pages_write")
+                                 *args, *((None, 0) if workspace is None else _space(workspace)), _stream(stream)), "squat_pages_write")
 
 
 def squat_pages_read(pool: PagePool, slots: torch.Tensor, k_out: torch.Tensor = None, v_out: torch.Tensor = None, stream=None):
@@ -823,7 +828,7 @@ def squat_chunk_attention(q: torch.Tensor, pool: PagePool, q_start: torch.Tensor
     _check(_direct().chunk_attention(
         softmax_scale, *_q_rows(q, "q"), pool.address, n_seqs, _int32(q_start, "q_start", n_seqs + 1), _int32(cached_len, "cached_len", n_seqs),
         _int32(page_table, "page_table", n_seqs * table[1]), table[1], *rows, *starts, max_q, 1 if causal else 0, *_rows(out, "out"),
-        None if lse is None else _dev(lse, "lse"), _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)),
+        None if lse is None else _dev(lse, "lse"), *_space(workspace), _stream(stream)),
         "squat_chunk_attention")
 
 

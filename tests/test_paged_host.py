@@ -276,3 +276,19 @@ def test_keys_and_values_that_are_read_into_one_place(lib):
     assert read(lib, k=A, v=A + 16) == INVALID                # a part of a row
     assert read(lib, k=A, kt=2048, v=A + 2048, vt=1024) == INVALID      # between each other's, with other strides
     assert read(lib, k=A, kt=2048, v=A + 2048 - 16, vt=2048) == INVALID
+
+
+def test_workspaces_with_holes(monkeypatch):
+    """What the kernels may write is the workspace's bytes in a row: views that have fewer, or others in between, are refused."""
+    class Calls:
+        def __getattr__(self, name):
+            return lambda *args: pytest.fail("called")
+
+    monkeypatch.setattr(sq.binding, "_direct", Calls)
+    monkeypatch.setattr(sq.binding, "_stream", lambda stream: None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for call, tensors in _fake_calls():
+        for bad in (_fake(1, dtype=torch.uint8).expand(4096), _fake(8192, dtype=torch.uint8)[::2]):
+            if "workspace" in tensors:
+                with pytest.raises(ValueError, match="contiguous"):
+                    call(**dict(tensors, workspace=bad))
