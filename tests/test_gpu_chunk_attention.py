@@ -368,3 +368,29 @@ def test_keys_and_queries_below_binary16(q_size, k_size, nq, rows, bits, G, meta
     assert bool(((out.double() - ref).abs() <= 8 * bound + 2.0 ** -8 * ref.abs()).all())
     assert ((out.double() - ref).norm() / ref.norm()).item() <= 2.0 ** -8 * 8 ** 0.5
     assert (lse.double() - ref_lse).abs().max().item() <= 0.02 * 8
+
+
+@pytest.mark.parametrize("bits, G, meta", [(2, 32, "f32"), (4, 32, "f32"), (2, 128, "f16"), (4, 64, "f16")])
+@pytest.mark.parametrize("heads, nq", [((2, 2), 1), ((8, 1), 1), ((8, 1), 2), ((8, 1), 3), ((8, 1), 16), ((8, 1), 40)])
+def test_scores_that_binary16_holds_exactly(bits, G, meta, heads, nq):
+    """Queries 0, 1/2 or 1 with either sign, scales 1/8 to 3/8, zero-points in 32nds below 8: keys have 9 bits, and products with a
+    scaled query and a code under its bias (up to 3/8 x 1039) are multiples of 2^-6 whose sums stay below 2^16, so binary16 and float32
+    hold them exactly, in every kernel.  What is left of lse's error, in powers of two of the exponent: the rounded softmax scale, its
+    product with a score and with the maximum, and their difference (below 32 each: 2^-19), one of 2^-21 for the exponential, 2^-24 for
+    each term of the sum, and 2^-22 of lse for the logarithm.  bf16 would be off by up to 2^-6 in a key."""
+    c, r = 7 * G, nq + 20
+    b = Batch(51 + nq, [(nq, c, r), (1, 2 * G, 3)], *heads, bits, G, meta, scale=0.04)
+    g = gen(bits + nq)
+    multiples = lambda lo, hi, of, x: (torch.randint(lo, hi, x.shape, generator=g, device="cuda") / of).to(x.dtype)  # noqa: E731
+    b.q = multiples(-2, 3, 2, b.q)
+    b.k_new.copy_(multiples(-16, 17, 8, b.k_new))
+    b.v_new.copy_(multiples(-16, 17, 8, b.v_new))
+    b.tensors[1], b.tensors[2] = multiples(1, 4, 8, b.tensors[1]), multiples(-255, 256, 32, b.tensors[2])
+    out, lse = call(b)
+    ref, ref_lse, _ = b.expected()
+    tol = (4 * 2.0 ** -19 + 2.0 ** -21 + (c + r) * 2.0 ** -24) * math.log(2) + 2.0 ** -22 * ref_lse.abs()
+    assert float((ref_lse * 1.4427).abs().max()) < 32
+    err = (lse.double() - ref_lse).abs()
+    print("lse off by", err.max().item(), "allowed", tol.min().item())
+    assert bool((err <= tol).all())
+    check(b, out, None)
