@@ -428,8 +428,10 @@ typedef struct {
  *   s         the layer's update matrices: keys as squat_quantize_keys, through `workspace` (device, 256-byte aligned, at
  *             least squat_pages_write_workspace_bytes(pool, n_tokens); nothing is kept in it between calls).  NULL: keys rounded
  *             to nearest without error feedback (W = 0), in one launch with the values and without a workspace.
- * Values, and keys with s = NULL: scale = (max - min) * RN(1 / L) in binary32 (a product, whose last bit may differ from the
- * quotient that squat_quantize_values and squat_quantize_keys store), zero = min; with meta16 both rounded to binary16.  Codes
+ * Values, and keys with s = NULL: scale = (max - min) * RN(1 / L) in binary32, zero = min; with meta16 both rounded to binary16.
+ * (A product: its last bit may differ from the quotient that squat_quantize_values and squat_quantize_keys store.  Where x lies
+ * within L 2^-22 steps of the middle between two levels, the code may then be the neighbour of theirs; either is as near, but what
+ * is read back differs by a step.  Caches that are to agree bit by bit take their values from the same entry point.)  Codes
  * are decided by the stored grid: values as c = clamp(rint((x - zero) / scale), 0, L) in binary32, operation by operation, keys as real
  * arithmetic would, ties to even.  n_tokens is a multiple of group_size.  Status word: as the quantizers set it.
  */
@@ -475,9 +477,10 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
  * Everything that changes from step to step is read on the device, so a captured call can be replayed with other lengths,
  * pages and row ranges (n_q, n_seqs and max_q as captured).  A length or row range outside its limits sets SQUAT_FLAG_PAGES and is
  * cut to them; for a page number outside the pool (the flag too) no page is read, and the result of that sequence is not defined.
- * Scores, softmax and sums are float32.  Keys, values, queries and weights enter the tensor cores in binary16 (11 significant
- * bits: codes, bf16 rows and queries exactly, dequantized values and weights rounded) where their magnitudes allow it, else in
- * bf16.
+ * Scores, softmax and sums are float32.  Keys, values, queries and weights enter the tensor cores in binary16 where their magnitudes
+ * allow it, else in bf16.  Binary16 has 11 significant bits from 2^-14 on: codes, bf16 rows and queries are exact there; scales and
+ * zero-points (float32 ones), dequantized keys and values and the softmax weights are rounded, and for up to 16 rows per KV head
+ * the product of a query and a key's scale in a dequantized key's place.
  */
 size_t squat_chunk_attention_workspace_bytes(int n_q, int n_q_heads, int n_kv_heads, int max_q);
 int squat_chunk_attention(const void *q, int n_q, int n_q_heads, long long q_stride_t, long long q_stride_h,

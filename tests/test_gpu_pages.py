@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2503_24358_b200 as sq
-from paged import D, META, deq_pool, gen, normal
+from paged import D, META, deq_pool, gen, normal, unpack
 
 pytestmark = pytest.mark.gpu
 
@@ -344,3 +344,24 @@ def test_keys_and_values_read_into_one_tensor(dtype):
                 sq.squat_pages_read(pool, slots, a, b)
                 assert torch.equal(a, ref[0]) and torch.equal(b, ref[1])
     assert min(found.values()) > 100, found
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bits, G", [(2, 32), (4, 64), (4, 128)])
+@pytest.mark.parametrize("kind", ["normal", "ties", "wide"])
+def test_codes_beside_those_of_a_contiguous_cache(dtype, bits, G, kind):
+    """Scales that differ in the last bit (2^-23 of themselves) move a border by at most L 2^-23 steps, and the float32 difference and
+    quotient of values round by 2^-24 of L steps each: codes differ by one, and only next to a border, where either level is as near."""
+    H, L, T = 3, 2 ** bits - 1, 5 * G
+    k, v, _ = inputs(T + bits, T, H, dtype, kind)
+    pool = sq.PagePool.empty(5, G, H, bits, G)
+    sq.squat_pages_write(pool, G * torch.arange(5, dtype=torch.int32, device="cuda"), k, v)
+    other = contiguous(sq.Subspace(H), k, v, bits, G, "f32")
+    dk, dv = deq_pool(pool.tensors, bits, G)
+    for x, d, codes in ((k, dk, other[0]), (v, dv, other[3])):
+        code, scale, zero = (d[n].transpose(1, 2).flatten(0, 1) for n in ("code", "scale", "zero"))
+        theirs = unpack(codes[0].transpose(0, 1), bits)
+        apart = (code - theirs).abs()
+        border = (torch.maximum(code, theirs) - 0.5 - (x.double() - zero) / scale).abs()
+        assert bool(((apart == 0) | ((apart == 1) & (border <= L * 2.0 ** -22))).all())
+        print(kind, "codes that differ:", int((apart != 0).sum()), "of", apart.numel())
