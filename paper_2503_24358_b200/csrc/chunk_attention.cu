@@ -19,8 +19,9 @@
 //   - A step's codes and metadata come through shared memory by cp.async, a step ahead.
 // The loops are rolled where the registers allow it: straight-line code of a step, met once by a short sequence, takes longer to be
 // fetched than to be executed.
-// 64 sequences of up to 4096 tokens, one new token each, 32 heads with keys of their own, 2 bits: 233 us, 2.6 TB/s of codes and metadata; the issue slots bound it
-// (790 instructions for 32 tokens of a head).
+// 64 sequences of up to 4096 tokens, one new token each, 32 heads with keys of their own, 2 bits: 235 us, 2.6 TB/s of codes and metadata: 870
+// instructions for 32 tokens of a head, issued at 60 % of the slots by 14 warps an SM.  16 sequences of up to 8160 tokens, 24 rows for each
+// of 8 heads: 81 us, 1310 instructions, at 45 % of the slots: 255 registers leave 8 warps an SM, which wait for one another's latencies.
 // Binary16 keeps 11 significant bits, three more than bf16: the result's own rounding to bf16 is what is left.  Magnitudes
 // beyond its range (or values that all lie below 2^-8, where it would lose them, or keys and queries of which it would lose what
 // matters: chunk_too_low) are noticed on the way, and the segment is done again with bf16 operands.  Weights carry a factor of 2^8, so that those down to 2^-32 of the largest are not lost.
@@ -39,7 +40,8 @@ struct Stage {                                       // one step's part of the c
     static constexpr int KC = 0, VC = STEP * ROW, KS = 2 * STEP * ROW, KZ = KS + 4 * QUARTER, VS = KZ + 4 * QUARTER, VZ = VS + STEP * 4 * MS;
     static constexpr int BYTES = VZ + STEP * 4 * MS;
 };
-// CTAs to an SM, by registers
+// CTAs to an SM, by registers.  Four of 8 rows: 64 ragged sequences, 32 heads with keys of their own, 235 us (three 247); on 8 KV heads 89
+// (three 87).  Three of 16 rows: 16 sequences of up to 8160 tokens 87 us, with 400 to 500 bytes of spills a thread (two, without: 79).
 template <int NT>
 constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;
 
@@ -801,8 +803,9 @@ int launch_rows_tiles(const ChunkParams &p, int bits, int meta16, cudaStream_t s
 
 // The kernels of a call.  Sequences with at most FEW_ROWS rows per KV head go to the kernel for few rows (8 `eights` of them share an
 // item), the others to the kernel for many, in tiles of 128 or 256.  Both sides, us a call, 32 / 8 heads, 2 bits: 16 sequences of up to 8160
-// tokens, 16 rows 84 and 119, 24 rows 81 and 120, 32 rows (in a kernel for four times eight) 105 and 114, 48 rows 163 and 138; two
-// such sequences, 24 rows 53 and 47, 32 rows 69 and 46; 32 of 2048 tokens at 4 bits, 24 rows 69 and 86, 32 rows 89 and 83.
+// tokens, 16 rows 84 and 119, 24 rows 81 and 122, 32 rows (in an instance of four times eight rows, which is not built) 105 and 114, 48 rows
+// 163 and 138; two such sequences, 24 rows 54 and 47, 32 rows 69 and 46; 32 of 2048 tokens at 4 bits, 24 rows 69 and 86, 32 rows 89 and 83.
+// So the border lies lower for a few long sequences than for many; their number is not looked at.
 struct ChunkKernels {
     int eights;                                      // 0: no kernel for few rows
     int tiles;                                       // 0: no kernel for many rows
@@ -866,6 +869,8 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
     if (k.tiles) {
         many.min_rows = k.eights ? FEW_ROWS + 1 : 1;
         many.max_rows = 0x7fffffff;
+        // us a call, 32 / 8 heads: 256 new tokens over 1024 at min_tiles 2 / 4 / 8: 49 / 53 / 62, 1024 without a cache 80 / 80 / 89; 24 mixed
+        // sequences at start 0 / 1 / 2 / 4: 215 / 200 / 188 / 177, 8 chunks of 256 72 / 62 / 62 / 63, 2048 over 8192 483 / 495 / 483 / 479
         many.min_tiles = 4;
         many.start = 2;
         use_part(many, workspace, matrix_workers(k.tiles), 128 * k.tiles, 128, 1);
@@ -875,6 +880,9 @@ int squat_launch_chunk_attention(ChunkParams p, const squat_page_pool *pool, flo
     if (rc == SQUAT_OK && k.eights) {
         few.min_rows = 1;
         few.max_rows = k.tiles ? FEW_ROWS : 0x7fffffff;
+        // us a call: 16 sequences of up to 512 tokens at min_tiles 1 / 3 / 6 / 12: 24 / 22 / 25 / 35, one of 256 13.5 / 15.9 / 20 / 27, one of
+        // 32768 52 / 52 / 45 / 44; 64 of up to 4096, 32 heads with keys of their own, at start 0 / 1 / 2 / 4: 320 / 263 / 235 / 213, 24 rows
+        // of 16 sequences 85 / 84 / 81 / 80
         few.min_tiles = 3;
         few.start = 2;
         use_part(few, workspace, rows_workers(k.eights, pool->bits, pool->meta16), 8 * k.eights, STEP, WARPS);

@@ -13,7 +13,7 @@
 // Channels stand in the order that the dequantization leaves them in (the two codes 16 bits apart in a word are neighbours); the
 // queries are stored the same way and the result is put in order when it is written.
 // Magnitudes beyond binary16 are noticed on the way, and the segment is done again with bf16 operands.
-// 2048 new tokens over 8192 cached ones, 32 / 8 heads of 2 bits: 489 us, 630 TFLOP/s.  The products, the exponentials and
+// 2048 new tokens over 8192 cached ones, 32 / 8 heads of 2 bits: 484 us, 640 TFLOP/s.  The products, the exponentials and
 // shared memory at its 128 bytes a cycle each take 2048 cycles for 256 rows and a tile, and do not overlap in full (5450); with four producer warps it took 561 us.
 #include "chunk_attention.cuh"
 

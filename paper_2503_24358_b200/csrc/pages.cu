@@ -3,8 +3,8 @@
 //   Delta = (M - m) RN(1 / L),   c = clamp(rint((x - z) / Delta), 0, L),   x' = z + Delta c     (z = m; or both rounded to binary16)
 //
 // Delta is a product of binary32 numbers: its last bit may differ from the rounded quotient that the quantizers of contiguous
-// caches store.  Codes are decided by the stored grid, so this is no error of theirs.
-// over G tokens per channel (keys) or G channels per token (values).
+// caches store.  Codes are decided by the stored grid, so this is no error of theirs; within L 2^-22 steps of the middle between two
+// levels they may be the neighbours of a contiguous cache's.  M and m: over G tokens per channel (keys) or G channels per token (values).
 //
 // Keys: a group is G rows of 256 or 512 contiguous bytes.  16 threads hold a row, eight channels each, eight rows to a thread; the
 // minima of a thread's rows (bf16: of channel pairs, packed), of the halves of a warp, then of the group's 2 to 8 warps.  Values: a
@@ -15,9 +15,10 @@
 // differ by one level at most, so the difference of the packed words has a bit for every element that is open (structural with
 // bf16 data).  Those are decided one by one (patch).
 //
-// Bound: HBM (x is read once, codes and metadata are written once; a group's codes are one contiguous span of its page), and close
-// behind it the instructions of the codes.  131072 tokens of 8 heads, keys and values in bf16, 2 bits: 150 us, 4.4 TB/s; 65536
-// tokens of 32 heads read back as bf16: 250 us, 5.4 TB/s.
+// Bound: HBM (x is read once, codes and metadata are written once; a group's codes are one contiguous span of its page) for what is read
+// back: 65536 tokens of 32 heads as bf16 250 us, 5.4 TB/s.  Writes are at neither limit: 131072 tokens of 8 heads, keys and values in
+// bf16, 2 bits: 148 us, 4.5 TB/s, 64 % of the issue slots, 21 warps an SM (values alone 72 us).  With a handle: the key kernel (rank 8
+// 216 us, dense 331 us for these) into the workspace, 38 us to place its output, and the values: 327 and 443 us.
 #include <type_traits>
 #include "pages.cuh"
 
