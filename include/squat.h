@@ -480,7 +480,8 @@ int squat_pages_read(const squat_page_pool *pool, const int *slots, int n_tokens
  * Scores, softmax and sums are float32.  Keys, values, queries and weights enter the tensor cores in binary16 where their magnitudes
  * allow it, else in bf16.  Binary16 has 11 significant bits from 2^-14 on: codes, bf16 rows and queries are exact there; scales and
  * zero-points (float32 ones), dequantized keys and values and the softmax weights are rounded, and for up to 16 rows per KV head
- * the product of a query and a key's scale in a dequantized key's place.
+ * the product of a query and a key's scale in a dequantized key's place.  Below, it rounds by up to 2^-25: values beside others of
+ * 2^-8 and more are good to that, not to a part of themselves.
  */
 size_t squat_chunk_attention_workspace_bytes(int n_q, int n_q_heads, int n_kv_heads, int max_q);
 int squat_chunk_attention(const void *q, int n_q, int n_q_heads, long long q_stride_t, long long q_stride_h,
